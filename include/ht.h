@@ -323,6 +323,89 @@ int ht_skinny_gemm_packed(const void *a, const void *packed, int32_t M, int32_t 
 int ht_skinny_gemm(const void *a, const void *w, int32_t M, int32_t N, int32_t K, int32_t dtype, float *out,
                    void *scratch, size_t scratch_bytes, void *stream);
 
+/* ---- a batch of sequences over a paged cache ------------------------------------------------------------
+ * The operators of a verify step for several sequences at once, sampled or greedy, for callers that run their own layers:
+ * append, attention, (projections and LM head of the caller), sample, accept.  Keys and values of a layer lie in two pools of
+ * pages [n_pages, n_kv_heads, page_rows, head_dim]; slot j of sequence s is row j % page_rows of page page_table[s][j / page_rows].
+ * Pages may be shared (a forked prompt) as long as nothing is appended to them or moved in them.
+ * A pass brings rows row_start[s] .. row_start[s + 1] - 1 for sequence s; its i-th row takes slot len[s] + i, and no row's slot
+ * depends on another sequence.  All tables are DEVICE arrays read when the work runs, so every call is capturable and a captured
+ * call may be replayed over new contents; nothing is kept between calls.  Calls on different streams do not interfere unless their
+ * outputs, pages or scratch overlap.
+ * The host's numbers are bounds: a length above max_len counts as max_len, rows of a sequence past max_rows or `rows` are left out,
+ * an entry of the page table outside 0 .. n_pages - 1 is no page (its slots are seen by nobody and nothing is stored there).
+ * Output rows that belong to no sequence stay as they were.
+ * HT_EINVAL unless 1 <= seqs <= 65535, 1 <= max_rows <= HT_MAX_ROWS, rows >= 1, 0 <= max_len <= 2^30, head_dim even and <= 256,
+ * page_rows a power of two in 8 .. 4096, n_pages, table_width >= 1; HT_ECAPACITY unless max_len + max_rows <= table_width * page_rows. */
+typedef struct {
+  int32_t seqs, rows /* rows of all sequences in this pass, at most */, max_rows /* of one sequence, at most */;
+  int32_t max_len /* cached slots of a sequence before this pass, at most */;
+  int32_t n_kv_heads, head_dim, dtype;
+  int32_t page_rows, n_pages, table_width;
+  const int32_t *row_start /* [seqs + 1], not decreasing */, *len /* [seqs] */, *page_table /* [seqs, table_width] */;
+} ht_paged_batch;
+
+/* Depth and ancestor bits of the rows of every sequence's tree, as ht_paged_append and ht_paged_attention take them (ht_dynamic_tree
+ * leaves the same tables).  parent [rows]: -1 or an earlier row of the same sequence, counted from the sequence's first row (anything
+ * else counts as -1).  depth [rows]; anc [rows, HT_MAX_ROWS / 64]: bit u of a row is set if row u of its sequence is it or an
+ * ancestor. */
+int ht_tree_tables(const ht_paged_batch *batch, const int32_t *parent, int32_t *depth, uint64_t *anc, void *stream);
+
+/* What happens to a query or key head on its way: y = x / sqrt(mean(x^2) + eps) * gain over the head (gain NULL: y = x), then the
+ * first rot_dim entries turn in pairs, (a, b) -> amplitude (a cos t - b sin t, b cos t + a sin t), t = position * f_j, j = 0 ..
+ * rot_dim / 2 - 1: pairs (j, j + rot_dim / 2), or (2j, 2j + 1) when interleaved.  f_j = inv_freq[j] when given (scaled positions of
+ * any kind), else rope_base^(-2j / rot_dim).  float32 throughout, rounded once; angles in 64 bits. */
+typedef struct {
+  const void *q_gain, *k_gain;               /* device [head_dim] in the batch's dtype, or NULL */
+  float eps;
+  int32_t rot_dim /* even, 0 .. head_dim */, interleaved;
+  float rope_base;
+  const float *inv_freq;                     /* device [rot_dim / 2] or NULL */
+  float amplitude;
+} ht_head_turn;
+
+/* Queries and keys through `turn` at position len[s] + depth (depth NULL: the row's number in its sequence), keys and values into
+ * their slots.  q [rows, Hq, head_dim], k, v [rows, n_kv_heads, head_dim], consecutive rows *_stride elements apart (the parts of a
+ * fused projection need no copy); q_out may be q.  q NULL: keys and values only; k and v NULL: queries only. */
+int ht_paged_append(const ht_paged_batch *batch, const ht_head_turn *turn, int32_t Hq, const void *q, int64_t q_stride,
+                    const void *k, int64_t k_stride, const void *v, int64_t v_stride, const int32_t *depth, void *q_out,
+                    int64_t q_out_stride, void *k_pages, void *v_pages, void *stream);
+
+/* Attention of every row over the cached slots 0 .. len[s] - 1 of its sequence and over the rows of this pass that its bits in
+ * `anc` name (NULL: itself and the rows before it: a prompt's chunk, or one token), whose keys and values ht_paged_append has
+ * stored.  out [rows, Hq, head_dim] = softmax(scale q.k) v; scale 0 means 1 / sqrt(head_dim).  Keys and values that a row does not see do
+ * not matter, whatever they hold; a row that sees nothing is 0.  Softmax and sums in float32.  Query heads h / (Hq / n_kv_heads)
+ * share a key/value head.  scratch: device, 256-byte aligned, >= ht_paged_attention_scratch_bytes (0 for a bad batch), of this call alone
+ * while it runs. */
+size_t ht_paged_attention_scratch_bytes(const ht_paged_batch *batch, int32_t Hq);
+int ht_paged_attention(const ht_paged_batch *batch, int32_t Hq, const void *q, int64_t q_stride, const void *k_pages,
+                       const void *v_pages, const uint64_t *anc, float scale, void *out, int64_t out_stride, void *scratch,
+                       size_t scratch_bytes, void *stream);
+
+/* One token per row of logits [rows, V] (rows row_stride elements apart, HT_F32 or HT_BF16; NaN counts as -inf), drawn with u[row].
+ * e_i = exp((x_i - max x) / temperature).  In the order (x descending, index ascending), these filters keep, one after the other:
+ * the first top_k (<= 0: all); the shortest prefix whose sum of e is at least top_p times that of all still kept (>= 1: all, <= 0:
+ * the first); those with e_i >= min_p (<= 0: all, above 1 as 1).  The token is the first index whose running sum of kept e, in index
+ * order, exceeds u times their total (u < 0 as 0; u >= 1: the last one kept).  A temperature <= 0 or NaN takes the largest logit, lowest
+ * index first.  If the maximum is +inf only such entries count; a row of -inf gives token -1.  Sums are in 64 bits.
+ * temperature, top_k, top_p, min_p: DEVICE [rows], or NULL (1; off).  tokens [rows]; logprob [rows] or NULL: the logarithm of the
+ * token's share of what was kept (0 for the largest logit of a temperature <= 0, -inf for token -1).
+ * HT_EINVAL unless 1 <= rows <= 2^20 and 1 <= V <= HT_MAX_SAMPLE_VOCAB. */
+enum { HT_MAX_SAMPLE_VOCAB = 1 << 20 };
+int ht_sample_rows(const void *logits, int64_t row_stride, int32_t dtype, int32_t rows, int32_t V, const float *u,
+                   const float *temperature, const int32_t *top_k, const float *top_p, const float *min_p, int32_t *tokens,
+                   float *logprob, void *stream);
+
+/* Acceptance and compaction for every sequence, the rule of ht_accept_and_compact: from row 0 on, repeatedly the first child (lowest
+ * row) whose token equals answers[] (a sampled or greedy token) of the row so far, at most max_path rows with the first.  The rows
+ * of that path move to slots len[s], len[s] + 1, .. in the pools of all layers (layer l at k_pages + l * layer_stride elements).
+ * parent, tokens, answers [rows]; outputs, DEVICE: n_accepted, next_root (the answer after the last accepted row), new_len (len +
+ * n_accepted) [seqs]; path, accepted_tokens [seqs, max_path], -1 behind the last.  A sequence without rows accepts 0, next_root -1.
+ * `len` itself is not changed; no output may lie in len, row_start, parent, tokens or answers (HT_EINVAL). */
+int ht_paged_accept(const ht_paged_batch *batch, int32_t layers, int64_t layer_stride, void *k_pages, void *v_pages,
+                    const int32_t *parent, const int32_t *tokens, const int32_t *answers, int32_t max_path, int32_t *n_accepted,
+                    int32_t *path, int32_t *accepted_tokens, int32_t *next_root, int32_t *new_len, void *stream);
+
 /* For callers that cannot allocate device memory (code under HIP-graph capture, tight serving loops, harnesses
  * that forbid hipMalloc): `ht_skinny_gemm_packed` without a scratch argument.  The split-K partial sums go to a
  * device array of HT_NOALLOC_SCRATCH_BYTES that is part of the library image (every GPU the library runs on holds

@@ -20,6 +20,7 @@ HT_OK, HT_EINVAL, HT_ECAPACITY, HT_ETREE, HT_ESTATE, HT_EHIP, HT_EUNSUPPORTED = 
 HT_F32, HT_BF16 = 0, 1
 HT_MAX_TRANSFER, HT_MAX_TREE, HT_MAX_ROWS, HT_MAX_TOPK = 8, 128, 256, 64
 HT_MAX_LOOP_STEPS = 64
+HT_MAX_SAMPLE_VOCAB = 1 << 20
 (HT_BUF_DRAFT_LOGITS, HT_BUF_CANDIDATES, HT_BUF_TREE_TOKENS, HT_BUF_SAVED_HIDDEN, HT_BUF_TRANSFER_SRC,
  HT_BUF_K_CACHE, HT_BUF_V_CACHE, HT_BUF_PSEUDO, HT_BUF_ROOT, HT_BUF_FUSED_DRAFT_LOGITS,
  HT_BUF_FUSED_CANDIDATES, HT_BUF_CANDIDATE_LOGPROBS, HT_BUF_TREE_PARENT, HT_BUF_TREE_RANK) = range(14)
@@ -33,6 +34,8 @@ EXPORTS = [
     "ht_gate_up_pack", "ht_gate_up_silu_packed", "ht_set_dynamic_tree", "ht_candidate_logprobs", "ht_dynamic_tree",
     "ht_training_forward", "ht_kl_divergence_rows", "ht_skinny_gemm_packed_noalloc",
     "ht_training_workspace_bytes", "ht_training_forward_batched",
+    "ht_tree_tables", "ht_paged_append", "ht_paged_attention_scratch_bytes", "ht_paged_attention", "ht_sample_rows",
+    "ht_paged_accept",
 ]
 
 
@@ -51,6 +54,16 @@ class ht_weights(C.Structure):
                 ("w_gate", _PP), ("w_up", _PP), ("w_down", _PP), ("w_transfer", _PP)]
 
 
+class ht_paged_batch(C.Structure):
+    _fields_ = [(n, C.c_int32) for n in ("seqs", "rows", "max_rows", "max_len", "n_kv_heads", "head_dim", "dtype", "page_rows",
+                                         "n_pages", "table_width")] + [(n, C.c_void_p) for n in ("row_start", "len", "page_table")]
+
+
+class ht_head_turn(C.Structure):
+    _fields_ = [("q_gain", C.c_void_p), ("k_gain", C.c_void_p), ("eps", C.c_float), ("rot_dim", C.c_int32),
+                ("interleaved", C.c_int32), ("rope_base", C.c_float), ("inv_freq", C.c_void_p), ("amplitude", C.c_float)]
+
+
 class HTError(RuntimeError):
     def __init__(self, code: int, message: str):
         super().__init__(f"libht error {code}: {message}")
@@ -63,6 +76,7 @@ def _load() -> C.CDLL:
                           "there is no fallback path")
     lib = C.CDLL(LIB_PATH)
     i32p, f32p, vp, sz = C.POINTER(C.c_int32), C.POINTER(C.c_float), C.c_void_p, C.c_size_t
+    i32, i64, bp = C.c_int32, C.c_int64, C.POINTER(ht_paged_batch)
     sig = {
         "ht_workspace_bytes": (C.c_int, [C.POINTER(ht_config), C.POINTER(sz)]),
         "ht_init_model": (C.c_int, [C.POINTER(ht_config), C.POINTER(ht_weights), vp, sz, vp, C.POINTER(vp)]),
@@ -101,6 +115,12 @@ def _load() -> C.CDLL:
         "ht_weight_pack": (C.c_int, [vp, C.c_int32, C.c_int32, vp, vp]),
         "ht_skinny_gemm_packed": (C.c_int, [vp, vp, C.c_int32, C.c_int32, C.c_int32, vp, vp, sz, vp]),
         "ht_skinny_gemm_packed_noalloc": (C.c_int, [vp, vp, C.c_int32, C.c_int32, C.c_int32, vp, vp]),
+        "ht_tree_tables": (C.c_int, [bp, vp, vp, vp, vp]),
+        "ht_paged_append": (C.c_int, [bp, C.POINTER(ht_head_turn), i32, vp, i64, vp, i64, vp, i64, vp, vp, i64, vp, vp, vp]),
+        "ht_paged_attention_scratch_bytes": (sz, [bp, i32]),
+        "ht_paged_attention": (C.c_int, [bp, i32, vp, i64, vp, vp, vp, C.c_float, vp, i64, vp, sz, vp]),
+        "ht_sample_rows": (C.c_int, [vp, i64, i32, i32, i32, vp, vp, vp, vp, vp, vp, vp, vp]),
+        "ht_paged_accept": (C.c_int, [bp, i32, i64] + [vp] * 5 + [i32] + [vp] * 6),
     }
     for name, (res, args) in sig.items():
         fn = getattr(lib, name)
@@ -216,6 +236,191 @@ def ht_dynamic_tree(lp, cand, root, k, b, T, parent, depth, rank, anc, tokens, s
     tokens [T] int32 and anc [T, HT_MAX_ROWS // 64] int64."""
     _check(lib.ht_dynamic_tree(_ptr(lp), _ptr(cand), _ptr(root), k, b, T, _ptr(parent), _ptr(depth), _ptr(rank),
                                _ptr(anc), _ptr(tokens), _stream_ptr(stream)))
+
+
+# ------------------------------------------------------------------ a batch over pages
+def _bad(message: str) -> HTError:
+    return HTError(HT_EINVAL, message)
+
+
+def _need(t, name, dtype, shape, device, rows_only=False):
+    """The tensor's address, if it is what the call reads: type, shape, device, and contiguous (rows_only: within a row).  None
+    stays None."""
+    if t is None:
+        return None
+    if t.dtype != dtype or tuple(t.shape) != tuple(shape) or t.device != device:
+        raise _bad(f"{name} is {t.dtype} {tuple(t.shape)} on {t.device}, wanted {dtype} {tuple(shape)} on {device}")
+    if rows_only:
+        if t.shape[0] and not t[0].is_contiguous():
+            raise _bad(f"{name} is not contiguous within a row")
+    elif not t.is_contiguous():
+        raise _bad(f"{name} is not contiguous")
+    return t.data_ptr()
+
+
+def _run(device, stream, fn, *args) -> None:
+    """The call on `stream`, or on the current stream of the tensors' device, with that device current."""
+    if stream is not None and stream.device != device:
+        raise _bad(f"the stream is on {stream.device}, the tensors on {device}")
+    if torch.cuda.current_device() == device.index:
+        _check(fn(*args, _stream_ptr(stream)))
+    else:
+        with torch.cuda.device(device):
+            _check(fn(*args, _stream_ptr(stream)))
+
+
+def _empty(shape, dtype, device, stream):
+    """Memory for a call on `stream`: the allocator's, for that stream (what another stream has freed may still be in use there)."""
+    if stream is None:
+        return torch.empty(shape, dtype=dtype, device=device)
+    with torch.cuda.stream(stream):
+        return torch.empty(shape, dtype=dtype, device=device)
+
+
+_DTYPES = {torch.float32: HT_F32, torch.bfloat16: HT_BF16}
+
+
+class PagedBatch:
+    """The buffers that describe a batch of sequences over pages (`ht_paged_batch`): row_start [seqs + 1], length [seqs] and
+    page_table [seqs, width] (int32, read when the work runs: contents may change between calls), the shape of a layer's pools
+    k_pages, v_pages [n_pages, n_kv_heads, page_rows, head_dim] (a leading dimension of layers is fine) and the host's bounds: rows of
+    all sequences in a pass, of one sequence, and cached slots of one."""
+
+    def __init__(self, row_start, length, page_table, k_pages, v_pages, rows: int, max_rows: int, max_len: int):
+        if k_pages.device.type != "cuda":
+            raise _bad("the pages are not on a GPU")
+        if k_pages.dtype not in _DTYPES or k_pages.dim() not in (4, 5) or page_table.dim() != 2:
+            raise _bad("pages are [n_pages, n_kv_heads, page_rows, head_dim] of float32 or bfloat16, the page table [seqs, width]")
+        self.device, self.dtype, self.pool = k_pages.device, k_pages.dtype, tuple(k_pages.shape[-4:])
+        self.seqs, self.rows = page_table.shape[0], rows
+        c = self.c = ht_paged_batch()
+        c.seqs, c.rows, c.max_rows, c.max_len = self.seqs, rows, max_rows, max_len
+        c.n_pages, c.n_kv_heads, c.page_rows, c.head_dim = self.pool
+        c.dtype, c.table_width = _DTYPES[self.dtype], page_table.shape[1]
+        c.row_start = _need(row_start, "row_start", torch.int32, (self.seqs + 1,), self.device)
+        c.len = _need(length, "length", torch.int32, (self.seqs,), self.device)
+        c.page_table = _need(page_table, "page_table", torch.int32, page_table.shape, self.device)
+        self.ref = C.byref(c)
+        self.tensors = (row_start, length, page_table)          # kept alive
+
+    def pages(self, t, name):
+        return _need(t, name, self.dtype, self.pool, self.device)
+
+    def ints(self, t, name):
+        return _need(t, name, torch.int32, (self.rows,), self.device)
+
+    def heads(self, t, name):
+        """(address, elements from a row to the next) of [rows, heads, head_dim]."""
+        if t is None:
+            return None, 0
+        if t.dim() != 3:
+            raise _bad(f"{name} is not [rows, heads, head_dim]")
+        at = _need(t, name, self.dtype, (self.rows, t.shape[1], self.pool[3]), self.device, rows_only=True)
+        return at, t.stride(0) if self.rows > 1 else t.shape[1] * t.shape[2]
+
+
+def ht_tree_tables(batch: PagedBatch, parent, stream=None):
+    """(depth [rows] int32, anc [rows, HT_MAX_ROWS // 64] int64) of parent [rows] int32."""
+    if parent is None:
+        raise _bad("parent is None")
+    depth = _empty((batch.rows,), torch.int32, batch.device, stream)
+    anc = _empty((batch.rows, HT_MAX_ROWS // 64), torch.int64, batch.device, stream)
+    _run(batch.device, stream, lib.ht_tree_tables, batch.ref, batch.ints(parent, "parent"), depth.data_ptr(), anc.data_ptr())
+    return depth, anc
+
+
+def ht_paged_append(batch: PagedBatch, q, k, v, k_pages, v_pages, depth=None, q_gain=None, k_gain=None, eps=1e-6, rot=None,
+                    interleaved=False, rope_base=10000.0, inv_freq=None, amplitude=1.0, q_out=None, stream=None):
+    """q [rows, Hq, hd], k, v [rows, Hkv, hd] (slices of a fused projection are fine); q or (k, v) may be None.  rot: entries of a
+    head that turn (all when None).  Returns q_out (allocated when None; q itself is fine), None without q."""
+    hd = batch.pool[3]
+    rot = hd if rot is None else rot
+    if q is not None and q_out is None:
+        q_out = _empty(q.shape, q.dtype, q.device, stream)
+    (qp, qs), (kp, ks), (vp, vs), (op, os_) = (batch.heads(t, n) for t, n in ((q, "q"), (k, "k"), (v, "v"), (q_out, "q_out")))
+    if q is not None and q.shape != q_out.shape:
+        raise _bad("q_out has another shape than q")
+    for t, n in ((k, "k"), (v, "v")):
+        if t is not None and t.shape[1] != batch.pool[1]:
+            raise _bad(f"{n} has {t.shape[1]} heads, the pages {batch.pool[1]}")
+    turn = ht_head_turn(_need(q_gain, "q_gain", batch.dtype, (hd,), batch.device), _need(k_gain, "k_gain", batch.dtype, (hd,), batch.device),
+                        eps, rot, int(interleaved), rope_base, _need(inv_freq, "inv_freq", torch.float32, (rot // 2,), batch.device),
+                        amplitude)
+    _run(batch.device, stream, lib.ht_paged_append, batch.ref, C.byref(turn), batch.pool[1] if q is None else q.shape[1], qp, qs, kp, ks,
+         vp, vs, batch.ints(depth, "depth"), op, os_, batch.pages(k_pages, "k_pages"), batch.pages(v_pages, "v_pages"))
+    return q_out
+
+
+def ht_paged_attention_scratch_bytes(batch: PagedBatch, Hq: int) -> int:
+    return lib.ht_paged_attention_scratch_bytes(batch.ref, Hq)
+
+
+def ht_paged_attention_scratch(batch: PagedBatch, Hq: int, stream=None):
+    """Scratch of a size for `ht_paged_attention` (one for every call that may run at the same time)."""
+    return _empty((max(256, ht_paged_attention_scratch_bytes(batch, Hq)),), torch.uint8, batch.device, stream)
+
+
+def ht_paged_attention(batch: PagedBatch, q, k_pages, v_pages, anc=None, scale=None, out=None, scratch=None, stream=None):
+    """q [rows, Hq, hd]; anc [rows, HT_MAX_ROWS // 64] int64, or None for a chain.  Returns out [rows, Hq, hd] (allocated when
+    None, like scratch; rows of no sequence hold what they held)."""
+    if q is None:
+        raise _bad("q is None")
+    if out is None:
+        out = _empty(q.shape, q.dtype, q.device, stream)
+    (qp, qs), (op, os_) = batch.heads(q, "q"), batch.heads(out, "out")
+    if q.shape != out.shape:
+        raise _bad("out has another shape than q")
+    if scratch is None:
+        scratch = ht_paged_attention_scratch(batch, q.shape[1], stream)
+    if scratch.device != batch.device or not scratch.is_contiguous():
+        raise _bad("scratch is not contiguous memory of the batch's device")
+    _run(batch.device, stream, lib.ht_paged_attention, batch.ref, q.shape[1], qp, qs, batch.pages(k_pages, "k_pages"),
+         batch.pages(v_pages, "v_pages"), _need(anc, "anc", torch.int64, (batch.rows, HT_MAX_ROWS // 64), batch.device),
+         0.0 if scale is None else scale, op, os_, scratch.data_ptr(), scratch.numel() * scratch.element_size())
+    return out
+
+
+def ht_sample_rows(logits, u, temperature=None, top_k=None, top_p=None, min_p=None, tokens=None, logprob=None, stream=None):
+    """logits [rows, V] float32 or bfloat16 (rows may be strided), u, temperature, top_p, min_p [rows] float32, top_k [rows] int32.
+    Returns (tokens [rows] int32, logprob [rows] float32)."""
+    dev = logits.device
+    if dev.type != "cuda" or logits.dim() != 2 or logits.dtype not in _DTYPES or (logits.shape[1] > 1 and logits.stride(1) != 1):
+        raise _bad("logits are rows of float32 or bfloat16 on a GPU")
+    rows, V = logits.shape
+    if u is None:
+        raise _bad("u is None")
+    f, i = torch.float32, torch.int32
+    if tokens is None:
+        tokens = _empty((rows,), i, dev, stream)
+    if logprob is None:
+        logprob = _empty((rows,), f, dev, stream)
+    _run(dev, stream, lib.ht_sample_rows, logits.data_ptr(), logits.stride(0) if rows > 1 else V, _DTYPES[logits.dtype], rows, V,
+         _need(u, "u", f, (rows,), dev), _need(temperature, "temperature", f, (rows,), dev), _need(top_k, "top_k", i, (rows,), dev),
+         _need(top_p, "top_p", f, (rows,), dev), _need(min_p, "min_p", f, (rows,), dev), _need(tokens, "tokens", i, (rows,), dev),
+         _need(logprob, "logprob", f, (rows,), dev))
+    return tokens, logprob
+
+
+def ht_paged_accept(batch: PagedBatch, k_pages, v_pages, parent, tokens, answers, max_path, out=None, stream=None):
+    """k_pages, v_pages: the pools of all layers [layers, n_pages, Hkv, page_rows, hd], or of one; parent, tokens, answers [rows] int32.
+    Returns (n_accepted [seqs], path [seqs, max_path], accepted_tokens [seqs, max_path], next_root [seqs], new_len [seqs]) int32,
+    parts of `out`, int32 [3 seqs + 2 seqs max_path] (allocated when None)."""
+    layers = k_pages.shape[0] if k_pages.dim() == 5 else 1
+    shape = batch.pool if k_pages.dim() == 4 else (layers,) + batch.pool
+    kp, vp = _need(k_pages, "k_pages", batch.dtype, shape, batch.device), _need(v_pages, "v_pages", batch.dtype, shape, batch.device)
+    if parent is None or tokens is None or answers is None:
+        raise _bad("parent, tokens and answers are needed")
+    B, P = batch.seqs, max_path
+    if P < 1 or P > HT_MAX_ROWS:
+        raise _bad(f"max_path {P} outside 1..{HT_MAX_ROWS}")
+    if out is None:
+        out = _empty((3 * B + 2 * B * P,), torch.int32, batch.device, stream)
+    at = _need(out, "out", torch.int32, (3 * B + 2 * B * P,), batch.device)
+    _run(batch.device, stream, lib.ht_paged_accept, batch.ref, layers, k_pages.stride(0) if layers > 1 else 0, kp, vp,
+         batch.ints(parent, "parent"), batch.ints(tokens, "tokens"), batch.ints(answers, "answers"), P, at, at + 12 * B,
+         at + 12 * B + 4 * B * P, at + 4 * B, at + 8 * B)
+    n, root, length, path, emitted = out.split([B, B, B, B * P, B * P])
+    return n, path.view(B, P), emitted.view(B, P), root, length
 
 
 def ht_stream_read_probe(buf, sink, stream=None) -> int:

@@ -1798,4 +1798,127 @@ int ht_dynamic_tree(const float* lp, const int32_t* cand, const int32_t* root, i
   return HT_OK;
 }
 
+// ------------------------------------------------------------------------------------------------ a batch over pages
+namespace {
+int check_paged(const ht_paged_batch* b, PagedRows* out) {
+  if (!b || !b->row_start || !b->len || !b->page_table) return fail(HT_EINVAL, "NULL argument");
+  if (b->dtype != HT_F32 && b->dtype != HT_BF16) return fail(HT_EINVAL, "bad dtype");
+  if (b->seqs < 1 || b->seqs > 65535) return fail(HT_EINVAL, "seqs %d outside 1..65535", b->seqs);
+  if (b->max_rows < 1 || b->max_rows > HT_MAX_ROWS) return fail(HT_EINVAL, "max_rows %d outside 1..%d", b->max_rows, HT_MAX_ROWS);
+  if (b->rows < 1) return fail(HT_EINVAL, "rows must be positive");
+  if (b->max_len < 0 || b->max_len > (1 << 30)) return fail(HT_EINVAL, "max_len %d outside 0..2^30", b->max_len);
+  if (b->n_kv_heads < 1 || b->n_kv_heads > 65535 || b->head_dim < 2 || b->head_dim % 2 || b->head_dim > 256)
+    return fail(HT_EINVAL, "bad head shape");
+  if (b->page_rows < 8 || b->page_rows > 4096 || (b->page_rows & (b->page_rows - 1)))
+    return fail(HT_EINVAL, "page_rows %d is not a power of two in 8..4096", b->page_rows);
+  if (b->n_pages < 1 || b->table_width < 1) return fail(HT_EINVAL, "n_pages and table_width must be positive");
+  if ((int64_t)b->table_width * b->page_rows < (int64_t)b->max_len + b->max_rows)
+    return fail(HT_ECAPACITY, "a table of %d pages of %d rows is shorter than max_len + max_rows = %d", b->table_width, b->page_rows,
+                b->max_len + b->max_rows);
+  *out = PagedRows{b->seqs, b->rows, b->max_rows, b->max_len, b->n_kv_heads, b->head_dim, __builtin_ctz(b->page_rows), b->n_pages,
+                   b->table_width, b->row_start, b->len, b->page_table};
+  return HT_OK;
+}
+int check_heads(const ht_paged_batch* b, int32_t Hq) {
+  if (Hq < 1 || Hq > 65535 || Hq % b->n_kv_heads) return fail(HT_EINVAL, "%d query heads for %d key/value heads", Hq, b->n_kv_heads);
+  return HT_OK;
+}
+}  // namespace
+
+int ht_tree_tables(const ht_paged_batch* batch, const int32_t* parent, int32_t* depth, uint64_t* anc, void* stream) {
+  PagedRows b;
+  if (const int rc = check_paged(batch, &b)) return rc;
+  if (!parent || !depth || !anc) return fail(HT_EINVAL, "NULL argument");
+  HT_HIP(launch_tree_tables(b, parent, depth, anc, (hipStream_t)stream));
+  return HT_OK;
+}
+
+int ht_paged_append(const ht_paged_batch* batch, const ht_head_turn* turn, int32_t Hq, const void* q, int64_t q_stride,
+                    const void* k, int64_t k_stride, const void* v, int64_t v_stride, const int32_t* depth, void* q_out,
+                    int64_t q_out_stride, void* k_pages, void* v_pages, void* stream) {
+  PagedRows b;
+  if (const int rc = check_paged(batch, &b)) return rc;
+  if (const int rc = check_heads(batch, Hq)) return rc;
+  if (!turn || (!q && !k)) return fail(HT_EINVAL, "NULL argument");
+  if ((k == nullptr) != (v == nullptr)) return fail(HT_EINVAL, "k and v must both be given or both be NULL");
+  if (q && !q_out) return fail(HT_EINVAL, "q without q_out");
+  if (k && (!k_pages || !v_pages)) return fail(HT_EINVAL, "k and v without pages");
+  if (turn->rot_dim < 0 || turn->rot_dim % 2 || turn->rot_dim > b.hd)
+    return fail(HT_EINVAL, "rot_dim %d is not an even number in 0..%d", turn->rot_dim, b.hd);
+  if (!turn->inv_freq && !(turn->rope_base > 1.f)) return fail(HT_EINVAL, "rope_base must be > 1 without inv_freq");
+  if ((turn->q_gain || turn->k_gain) && !(turn->eps >= 0.f)) return fail(HT_EINVAL, "eps must be >= 0");
+  const int64_t qw = (int64_t)Hq * b.hd, kw = (int64_t)b.Hkv * b.hd;
+  if ((q && (q_stride < qw || q_out_stride < qw)) || (k && (k_stride < kw || v_stride < kw)))
+    return fail(HT_EINVAL, "a row stride is shorter than the row");
+  AppendRows a{};
+  a.q = q, a.k = k, a.v = v, a.q_stride = q_stride, a.k_stride = k_stride, a.v_stride = v_stride, a.q_out_stride = q_out_stride;
+  a.q_out = q_out, a.k_pages = k_pages, a.v_pages = v_pages, a.q_gain = turn->q_gain, a.k_gain = turn->k_gain, a.depth = depth;
+  a.inv_freq = turn->inv_freq, a.eps = turn->eps, a.amplitude = turn->amplitude, a.Hq = Hq, a.rot = turn->rot_dim;
+  a.interleaved = turn->interleaved != 0;
+  if (!a.inv_freq && a.rot) a.step = rope_step(turn->rope_base, a.rot / 2);
+  HT_HIP(launch_paged_append(batch->dtype, b, a, (hipStream_t)stream));
+  return HT_OK;
+}
+
+size_t ht_paged_attention_scratch_bytes(const ht_paged_batch* batch, int32_t Hq) {
+  PagedRows b;
+  if (check_paged(batch, &b) || check_heads(batch, Hq)) return 0;
+  return align_up(paged_attn_scratch_bytes(batch->dtype, b, Hq) + 1, 256);
+}
+
+int ht_paged_attention(const ht_paged_batch* batch, int32_t Hq, const void* q, int64_t q_stride, const void* k_pages,
+                       const void* v_pages, const uint64_t* anc, float scale, void* out, int64_t out_stride, void* scratch,
+                       size_t scratch_bytes, void* stream) {
+  PagedRows b;
+  if (const int rc = check_paged(batch, &b)) return rc;
+  if (const int rc = check_heads(batch, Hq)) return rc;
+  if (!q || !k_pages || !v_pages || !out || !scratch) return fail(HT_EINVAL, "NULL argument");
+  if (!(scale >= 0.f) || scale > 1e30f) return fail(HT_EINVAL, "scale must be a finite number, 0 for 1 / sqrt(head_dim)");
+  if (q_stride < (int64_t)Hq * b.hd || out_stride < (int64_t)Hq * b.hd) return fail(HT_EINVAL, "a row stride is shorter than the row");
+  if (scratch_bytes < ht_paged_attention_scratch_bytes(batch, Hq)) return fail(HT_EINVAL, "scratch too small");
+  if ((uintptr_t)scratch % 256) return fail(HT_EINVAL, "scratch must be 256-byte aligned");
+  const double s = scale > 0.f ? (double)scale : 1.0 / sqrt((double)b.hd);
+  AttnRows a{q, k_pages, v_pages, q_stride, out_stride, anc, out, (float)(s * 1.4426950408889634), Hq};
+  HT_HIP(launch_paged_attn(batch->dtype, b, a, scratch, (hipStream_t)stream));
+  return HT_OK;
+}
+
+int ht_sample_rows(const void* logits, int64_t row_stride, int32_t dtype, int32_t rows, int32_t V, const float* u,
+                   const float* temperature, const int32_t* top_k, const float* top_p, const float* min_p, int32_t* tokens,
+                   float* logprob, void* stream) {
+  if (!logits || !u || !tokens) return fail(HT_EINVAL, "NULL argument");
+  if (dtype != HT_F32 && dtype != HT_BF16) return fail(HT_EINVAL, "bad dtype");
+  if (rows < 1 || rows > (1 << 20) || V < 1 || V > HT_MAX_SAMPLE_VOCAB || row_stride < V)
+    return fail(HT_EINVAL, "bad shape rows=%d V=%d row_stride=%lld", rows, V, (long long)row_stride);
+  SampleRows a{logits, row_stride, rows, V, u, temperature, top_p, min_p, top_k, tokens, logprob};
+  HT_HIP(launch_sample_rows(dtype, a, (hipStream_t)stream));
+  return HT_OK;
+}
+
+int ht_paged_accept(const ht_paged_batch* batch, int32_t layers, int64_t layer_stride, void* k_pages, void* v_pages,
+                    const int32_t* parent, const int32_t* tokens, const int32_t* answers, int32_t max_path, int32_t* n_accepted,
+                    int32_t* path, int32_t* accepted_tokens, int32_t* next_root, int32_t* new_len, void* stream) {
+  PagedRows b;
+  if (const int rc = check_paged(batch, &b)) return rc;
+  if (!k_pages || !v_pages || !parent || !tokens || !answers || !n_accepted || !path || !accepted_tokens || !next_root || !new_len)
+    return fail(HT_EINVAL, "NULL argument");
+  if (layers < 1 || layers > 65535) return fail(HT_EINVAL, "layers %d outside 1..65535", layers);
+  if (max_path < 1 || max_path > HT_MAX_ROWS) return fail(HT_EINVAL, "max_path %d outside 1..%d", max_path, HT_MAX_ROWS);
+  const int64_t pool = (int64_t)b.n_pages * b.Hkv * batch->page_rows * b.hd;
+  if (layers > 1 && layer_stride < pool) return fail(HT_EINVAL, "a layer stride is shorter than the pool");
+  // every workgroup reads the lengths and the trees: what one of them writes may not lie there
+  const struct { const void* p; size_t ints; } in[5] = {{b.len, (size_t)b.seqs}, {b.row_start, (size_t)b.seqs + 1}, {parent, (size_t)b.rows},
+                                                        {tokens, (size_t)b.rows}, {answers, (size_t)b.rows}},
+      to[5] = {{n_accepted, (size_t)b.seqs}, {path, (size_t)b.seqs * max_path}, {accepted_tokens, (size_t)b.seqs * max_path},
+               {next_root, (size_t)b.seqs}, {new_len, (size_t)b.seqs}};
+  for (const auto& o : to)
+    for (const auto& i : in)
+      if ((uintptr_t)o.p < (uintptr_t)i.p + 4 * i.ints && (uintptr_t)i.p < (uintptr_t)o.p + 4 * o.ints)
+        return fail(HT_EINVAL, "an output lies in len, row_start, parent, tokens or answers");
+  AcceptRows a{k_pages, v_pages, layers > 1 ? (size_t)layer_stride : (size_t)0, parent, tokens, answers, max_path, n_accepted, path,
+               accepted_tokens, next_root, new_len};
+  HT_HIP(launch_paged_accept(batch->dtype, b, a, layers, (hipStream_t)stream));
+  return HT_OK;
+}
+
 }  // extern "C"

@@ -70,6 +70,12 @@ __device__ inline double2 rope_turns(int j, double2 step) {      // base^(-2j/hd
   const double t_rest = fma(e, per_turn, -t) + fma(e, per_turn_rest, e_rest * per_turn);
   return make_double2(ldexp(t, (int)k), ldexp(t_rest, (int)k));
 }
+// the same of a frequency that is given: one over 2 pi times it, in two doubles
+__device__ inline double2 freq_turns(float freq) {
+  constexpr double per_turn = 0.15915494309189535, per_turn_rest = -9.8393383375912429e-18;
+  const double f = (double)freq, t = f * per_turn;
+  return make_double2(t, fma(f, per_turn, -t) + f * per_turn_rest);
+}
 __device__ inline float2 rope_factor(int pos, double2 turns) {
 #pragma clang fp contract(off)
   // (u rounded: its rest is added below, and a product fused into the subtraction would count it twice)
@@ -329,5 +335,69 @@ hipError_t launch_attn_causal(const void* q, const void* kc, const void* vc, int
                               int hd, void* out, hipStream_t s, const void* self_k = nullptr, const void* self_v = nullptr,
                               int self_cap = 0, void* scratch = nullptr);
 size_t attn_causal_scratch_bytes(int rows, int Hq, int hd);
+
+// ------------------------------------------------------------------------------------------------ a batch over pages
+// Keys and values in pages [n_pages][Hkv][1 << page_shift][hd]; slot j of sequence s lies in page table[s][j >> page_shift].
+struct PagedRows {
+  int32_t seqs, rows, max_rows, max_len, Hkv, hd, page_shift, n_pages, table_width;
+  const int32_t *row_start, *len, *table;
+};
+// What a sequence has in a pass: its first row, rows and cached slots, whatever the device's tables say within the host's bounds
+struct SeqSpan {
+  int row0, count, n;
+};
+__device__ inline SeqSpan seq_span(const PagedRows& b, int seq) {
+  auto held = [](int v, int hi) { return v < 0 ? 0 : v > hi ? hi : v; };
+  const int r0 = held(b.row_start[seq], b.rows), r1 = held(b.row_start[seq + 1], b.rows);
+  return SeqSpan{r0, held(r1 - r0, b.max_rows), held(b.len[seq], b.max_len)};
+}
+// The page of a slot below max_len + max_rows, -1 where the table names none of the pool's
+__device__ inline int page_of(const PagedRows& b, int seq, int slot) {
+  const int id = b.table[(size_t)seq * b.table_width + (slot >> b.page_shift)];
+  return (unsigned)id < (unsigned)b.n_pages ? id : -1;
+}
+hipError_t launch_tree_tables(const PagedRows& b, const int32_t* parent, int32_t* depth, uint64_t* anc, hipStream_t s);
+// Rows [rows][heads][hd], a row `*_stride` elements behind the one before; q or (k, v) may be NULL
+struct AppendRows {
+  const void *q, *k, *v;
+  int64_t q_stride, k_stride, v_stride, q_out_stride;
+  void *q_out, *k_pages, *v_pages;
+  const void *q_gain, *k_gain;               // NULL: no norm
+  const int32_t* depth;                      // NULL: a chain
+  const float* inv_freq;                     // NULL: frequencies of the base behind `step`
+  double2 step;                              // rope_step
+  float eps, amplitude;
+  int32_t Hq, rot, interleaved;
+};
+hipError_t launch_paged_append(int dtype, const PagedRows& b, const AppendRows& a, hipStream_t s);
+struct AttnRows {
+  const void *q, *k_pages, *v_pages;
+  int64_t q_stride, out_stride;
+  const uint64_t* anc;                       // NULL: a chain
+  void* out;
+  float scale_log2;                          // scale / ln 2
+  int32_t Hq;
+};
+size_t paged_attn_scratch_bytes(int dtype, const PagedRows& b, int Hq);
+hipError_t launch_paged_attn(int dtype, const PagedRows& b, const AttnRows& a, void* scratch, hipStream_t s);
+struct AcceptRows {
+  void *k_pages, *v_pages;
+  size_t layer_elems;                        // from a layer's pool to the next
+  const int32_t *parent, *tokens, *answers;
+  int32_t max_path;
+  int32_t *accepted, *path, *emitted, *next_root, *new_len;
+};
+hipError_t launch_paged_accept(int dtype, const PagedRows& b, const AcceptRows& a, int layers, hipStream_t s);
+// One token per row of logits (ht_sample.hip)
+struct SampleRows {
+  const void* z;
+  int64_t stride;
+  int32_t rows, V;
+  const float *u, *temperature, *top_p, *min_p;
+  const int32_t* top_k;
+  int32_t* tokens;
+  float* logprob;
+};
+hipError_t launch_sample_rows(int dtype, const SampleRows& a, hipStream_t s);
 
 }  // namespace ht
