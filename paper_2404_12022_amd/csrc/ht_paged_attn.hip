@@ -73,13 +73,565 @@ __global__ __launch_bounds__(64) void paged_attn_simple_kernel(PagedRows b, Attn
     if (lane + 64 * t < hd) Conv<T>::store(out + lane + 64 * t, sum == 0.f ? 0.f : acc[t] * inv);
 }
 
-size_t paged_attn_scratch_bytes(int, const PagedRows&, int) { return 0; }
+// ------------------------------------------------------------------------------------------------ bf16, heads of 64 and 128
+// The matrix-core kernels work transposed, a column being a (row, query head of the group) pair of one sequence and key/value head:
+//   S^T[key][col] = K[key][:] . Q[col][:]      O^T[e][col] += V^T[e][key] P[key][col]
+// The 32 keys of a block are assigned to the two 16-row score products in the order key = 8 (r / 4) + 4 b + r % 4, so the eight scores
+// a lane holds are the eight consecutive keys that its P operand of the second product wants.  V lies in its pages as rows of a
+// key (one row is stored and moved as one piece); its way through LDS ends in transposing reads, four keys of one column e at a time.
+namespace {
 
-hipError_t launch_paged_attn(int dtype, const PagedRows& b, const AttnRows& a, void*, hipStream_t s) {
-  const dim3 grid(a.Hq, b.max_rows, b.seqs);
-  if (dtype == 0) hipLaunchKernelGGL(paged_attn_simple_kernel<float>, grid, dim3(64), 0, s, b, a);
-  else hipLaunchKernelGGL(paged_attn_simple_kernel<bf16_t>, grid, dim3(64), 0, s, b, a);
+typedef __bf16 bf16x8_t __attribute__((ext_vector_type(8)));
+typedef float floatx4_t __attribute__((ext_vector_type(4)));
+typedef unsigned int u32x4_t __attribute__((ext_vector_type(4)));
+typedef short s16x4_t __attribute__((ext_vector_type(4)));
+
+union Frag {
+  u32x4_t nat;
+  bf16x8_t v;
+  uint2 half[2];
+  uint32_t u[4];
+};
+// 16 and 8 bytes at any address (a caller's rows need not lie on 16)
+struct __attribute__((packed, aligned(2))) Loose16 {
+  u32x4_t v;
+};
+struct __attribute__((packed, aligned(2))) Loose8 {
+  uint2 v;
+};
+
+constexpr float kRescaleStep = 8.0f;         // log2 units the reference point may lag behind the maximum: probabilities stay below 2^8
+
+__device__ __forceinline__ float max_over_groups(float x) {
+  auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  x = fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+  auto r2 = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  return fmaxf(__uint_as_float(r2[0]), __uint_as_float(r2[1]));
+}
+__device__ __forceinline__ float sum_over_groups(float x) {
+  auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  x = __uint_as_float(r[0]) + __uint_as_float(r[1]);
+  auto r2 = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  return __uint_as_float(r2[0]) + __uint_as_float(r2[1]);
+}
+
+// Where the 16-byte piece of a key's row lies in LDS, in bytes from the row's start.  K is read 16 rows of one piece at a time (a
+// quarter of a wavefront; rows 8 apart and 0 .. 3), V 16 rows of one 32-byte unit: both are spread over the 256 bytes of all banks.
+template <int HD> __device__ __forceinline__ int k_place(int row, int piece) {
+  const int h = HD == 128 ? (row & 3) | ((row >> 3) & 3) << 2 : ((row >> 1) & 1) | ((row >> 3) & 3) << 1;
+  return (piece ^ h) << 4;
+}
+template <int HD> __device__ __forceinline__ int v_place(int row, int unit) {
+  const int f = HD == 128 ? (row & 3) | ((row >> 3) & 1) << 2 : ((row >> 1) & 1) | ((row >> 3) & 1) << 1;
+  return (unit ^ f) << 5;
+}
+// V^T operand of 32 keys: rows e = eb * 16 + r16, keys 8 g .. 8 g + 7
+template <int HD> __device__ __forceinline__ Frag v_operand(const unsigned char* rows, int eb, int r16, int g) {
+  Frag f;
+#pragma unroll
+  for (int h = 0; h < 2; ++h) {
+    const int row = 8 * g + 4 * h + (r16 >> 2);
+    const unsigned char* at = rows + row * (HD * 2) + v_place<HD>(row, eb) + (r16 & 3) * 8;
+    const s16x4_t x = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4_t*)at);
+    f.half[h] = *(const uint2*)&x;
+  }
+  return f;
+}
+
+// Columns of a wavefront: QB blocks of 16
+template <int HD, int QB> struct Columns {
+  static constexpr int ES = HD / 32, EB = HD / 16;
+  Frag q[QB][ES];
+  floatx4_t o[QB][EB];
+  float m[QB], l[QB];                        // reference point (log2 units, scaled) and this lane's part of the sum
+  int row[QB], head[QB];                     // row of the sequence (count or more: none) and query head
+
+  __device__ __forceinline__ void start(const AttnRows& a, const SeqSpan& sp, int hk, int group, int col0, int r16, int g) {
+#pragma unroll
+    for (int qb = 0; qb < QB; ++qb) {
+      const int c = col0 + qb * 16 + r16;
+      row[qb] = c / group;
+      head[qb] = hk * group + c % group;
+      const int r = row[qb] < sp.count ? row[qb] : sp.count - 1;
+      const bf16_t* src = (const bf16_t*)a.q + (int64_t)(sp.row0 + r) * a.q_stride + (int64_t)head[qb] * HD + g * 8;
+#pragma unroll
+      for (int es = 0; es < ES; ++es) q[qb][es].nat = ((const Loose16*)(src + es * 32))->v;
+      m[qb] = -INFINITY;
+      l[qb] = 0.f;
+#pragma unroll
+      for (int eb = 0; eb < EB; ++eb) o[qb][eb] = floatx4_t{0.f, 0.f, 0.f, 0.f};
+    }
+  }
+
+  // Keys j0 .. j0 + 63 that column block qb sees, as bits; `there`: those that are
+  __device__ __forceinline__ uint64_t seen(const AttnRows& a, const SeqSpan& sp, int qb, int j0, uint64_t there) const {
+    const int first = j0 - sp.n;                           // the row of the pass that key j0 is
+    if (first <= -64 || row[qb] >= sp.count) return there;
+    uint64_t bits;
+    if (!a.anc) {
+      const int upto = row[qb] - first;                    // rows 0 .. row
+      bits = upto < 0 ? 0ull : upto >= 63 ? ~0ull : (2ull << upto) - 1;
+    } else {
+      const uint64_t* w = a.anc + (size_t)(sp.row0 + row[qb]) * kMaskWords;
+      if (first < 0) {
+        bits = w[0] << -first | ((1ull << -first) - 1);
+      } else {
+        const int i = first >> 6, s = first & 63;
+        bits = i < kMaskWords ? w[i] >> s : 0ull;
+        if (s && i + 1 < kMaskWords) bits |= w[i + 1] << (64 - s);
+      }
+    }
+    return bits & there;
+  }
+
+  // SUB blocks of 32 keys: k(sub, block, piece) their K operands, V rows in LDS, and with MASKED what every column sees of them
+  template <int SUB, bool MASKED, typename K>
+  __device__ __forceinline__ void multiply(K&& k, const unsigned char* v_rows, const uint64_t (&vis)[QB], float scale, int r16, int g) {
+    float p[QB][8 * SUB];
+#pragma unroll
+    for (int sub = 0; sub < SUB; ++sub)
+#pragma unroll
+      for (int b = 0; b < 2; ++b) {
+        Frag kf[ES];
+#pragma unroll
+        for (int es = 0; es < ES; ++es) kf[es] = k(sub, b, es);
+#pragma unroll
+        for (int qb = 0; qb < QB; ++qb) {
+          floatx4_t s = floatx4_t{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+          for (int es = 0; es < ES; ++es) s = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf[es].v, q[qb][es].v, s, 0, 0, 0);
+#pragma unroll
+          for (int i = 0; i < 4; ++i) p[qb][sub * 8 + b * 4 + i] = s[i];
+        }
+      }
+#pragma unroll
+    for (int qb = 0; qb < QB; ++qb) {
+      if (MASKED) {
+#pragma unroll
+        for (int x = 0; x < 8 * SUB; ++x) {
+          const uint32_t word = (uint32_t)(vis[qb] >> (x >> 3) * 32) >> g * 8;
+          p[qb][x] = word >> (x & 7) & 1 ? p[qb][x] : -INFINITY;
+        }
+      }
+      float top = p[qb][0];
+#pragma unroll
+      for (int x = 1; x < 8 * SUB; ++x) top = fmaxf(top, p[qb][x]);
+      top = max_over_groups(top) * scale;
+      const bool grow = top > m[qb] + kRescaleStep;        // m = -inf: any number
+      if (__any(grow)) {
+        const float keep = grow ? __builtin_amdgcn_exp2f(m[qb] - top) : 1.0f;
+        l[qb] *= keep;
+#pragma unroll
+        for (int eb = 0; eb < EB; ++eb) o[qb][eb] *= keep;
+        m[qb] = grow ? top : m[qb];
+      }
+      const float ref = m[qb] == -INFINITY ? 0.f : m[qb];
+      float sum = 0.f;
+#pragma unroll
+      for (int x = 0; x < 8 * SUB; ++x) {
+        p[qb][x] = __builtin_amdgcn_exp2f(fmaf(p[qb][x], scale, -ref));
+        sum += p[qb][x];
+      }
+      l[qb] += sum;
+    }
+#pragma unroll
+    for (int sub = 0; sub < SUB; ++sub) {
+      Frag pf[QB];
+#pragma unroll
+      for (int qb = 0; qb < QB; ++qb)
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+          pf[qb].half[h] = pack4_bf16(p[qb][sub * 8 + 4 * h], p[qb][sub * 8 + 4 * h + 1], p[qb][sub * 8 + 4 * h + 2], p[qb][sub * 8 + 4 * h + 3]);
+      const unsigned char* rows = v_rows + sub * 32 * HD * 2;
+      bool odd = false;
+#pragma unroll
+      for (int eb = 0; eb < EB; ++eb) {
+        Frag vf = v_operand<HD>(rows, eb, r16, g);
+        if (MASKED) {                                      // a value that is no number would reach columns that do not see it
+#pragma unroll
+          for (int w = 0; w < 4; ++w) {
+            const bool lo = (vf.u[w] & 0x7f80u) == 0x7f80u, hi = (vf.u[w] & 0x7f800000u) == 0x7f800000u;
+            odd |= lo | hi;
+            vf.u[w] &= (lo ? 0u : 0xffffu) | (hi ? 0u : 0xffff0000u);
+          }
+        }
+#pragma unroll
+        for (int qb = 0; qb < QB; ++qb) o[qb][eb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf.v, pf[qb].v, o[qb][eb], 0, 0, 0);
+      }
+      if (MASKED && __any(odd)) add_odd<SUB>(p, sub, rows, r16, g);
+    }
+  }
+  // The values of 32 keys that are no numbers, to the columns that see them: rare, key by key
+  template <int SUB>
+  __device__ __forceinline__ void add_odd(const float (&p)[QB][8 * SUB], int sub, const unsigned char* rows, int r16, int g) {
+#pragma unroll 1
+    for (int key = 0; key < 32; ++key) {
+      float w[QB];
+#pragma unroll
+      for (int qb = 0; qb < QB; ++qb) {
+        float mine = 0.f;
+#pragma unroll
+        for (int x = 0; x < 8; ++x) mine = (key & 7) == x ? p[qb][sub * 8 + x] : mine;
+        w[qb] = __shfl(mine, (key >> 3) * 16 + r16, 64);
+      }
+#pragma unroll
+      for (int eb = 0; eb < EB; ++eb) {
+        const uint2 four = *(const uint2*)(rows + key * (HD * 2) + v_place<HD>(key, eb) + g * 8);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const uint32_t v = (i < 2 ? four.x : four.y) >> (i & 1) * 16 & 0xffffu;
+          if ((v & 0x7f80u) == 0x7f80u) {
+#pragma unroll
+            for (int qb = 0; qb < QB; ++qb)
+              if (w[qb] != 0.f) o[qb][eb][i] += w[qb] * __uint_as_float(v << 16);
+          }
+        }
+      }
+    }
+  }
+
+  // Column (qb, r16): o and the sum over its four lanes, to `out` or to the split's partial results
+  __device__ __forceinline__ void finish(const AttnRows& a, const SeqSpan& sp, int qb, const floatx4_t& acc, int eb, float sum, int g,
+                                         float* part_o) const {
+    if (row[qb] >= sp.count) return;
+    const int64_t at = (int64_t)(sp.row0 + row[qb]);
+    const int e0 = eb * 16 + g * 4;
+    if (part_o) {
+      *(float4*)(part_o + (at * a.Hq + head[qb]) * HD + e0) = make_float4(acc[0], acc[1], acc[2], acc[3]);
+    } else {
+      const float inv = sum == 0.f ? 0.f : 1.0f / sum;
+      ((Loose8*)((bf16_t*)a.out + at * a.out_stride + (int64_t)head[qb] * HD + e0))->v =
+          sum == 0.f ? make_uint2(0, 0) : pack4_bf16(acc[0] * inv, acc[1] * inv, acc[2] * inv, acc[3] * inv);
+    }
+  }
+  __device__ __forceinline__ void finish_sum(const AttnRows& a, const SeqSpan& sp, int qb, float top, float sum, float* part_ml) const {
+    if (row[qb] < sp.count) *(float2*)(part_ml + ((int64_t)(sp.row0 + row[qb]) * a.Hq + head[qb]) * 2) = make_float2(top, sum);
+  }
+};
+
+// A sequence's share of a split launch: keys key0 .. key1 - 1
+struct Slice {
+  int key0, key1, count;
+};
+__device__ __forceinline__ Slice slice_of(const SeqSpan& sp, int split, int split_len) {
+  const int S = sp.n + sp.count;
+  const int count = (S + split_len - 1) / split_len, k0 = split * split_len;
+  return Slice{k0, k0 + split_len < S ? k0 + split_len : S, count};
+}
+
+}  // namespace
+
+// Up to 32 columns: the four wavefronts of a workgroup take blocks of 32 keys in turn, each for itself (no barrier until the end),
+// K from global memory straight into operand registers, V through 32 rows of LDS of the wavefront's own; the next block is in
+// flight while one is multiplied.  Bound by what the cache streams at.
+template <int HD, int QB>
+__global__ __launch_bounds__(256, 2) void paged_attn_few_kernel(PagedRows b, AttnRows a, int split_len, float* part_o, float* part_ml) {
+  using Cols = Columns<HD, QB>;
+  constexpr int ES = Cols::ES, EB = Cols::EB, PIECES = HD / 8, LOADS = 32 * PIECES / 64, V_BYTES = 32 * HD * 2, STEP = 4 * 32;
+  constexpr int O_FLOATS = EB * 4 * 64;
+  __shared__ __attribute__((aligned(1024))) unsigned char lds[4 * V_BYTES > 4 * O_FLOATS * 4 ? 4 * V_BYTES : 4 * O_FLOATS * 4];
+  __shared__ float lds_m[4 * 64], lds_l[4 * 64];
+  const int seq = blockIdx.z, hk = blockIdx.x, group = a.Hq / b.Hkv, split = blockIdx.y;
+  const SeqSpan sp = seq_span(b, seq);
+  const Slice sl = slice_of(sp, split, split_len);
+  if (sp.count == 0 || sl.key0 >= sl.key1) return;
+  const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, r16 = lane & 15, g = lane >> 4;
+  const int S = sp.n + sp.count, in_page = (1 << b.page_shift) - 1;
+  const size_t page_elems = (size_t)b.Hkv * HD << b.page_shift, head_elems = (size_t)hk * HD << b.page_shift;
+  const int32_t* table = b.table + (size_t)seq * b.table_width;
+  const bf16_t *kp = (const bf16_t*)a.k_pages + head_elems, *vp = (const bf16_t*)a.v_pages + head_elems;
+  unsigned char* v_rows = lds + wave * V_BYTES;
+
+  Cols cols;
+  cols.start(a, sp, hk, group, 0, r16, g);
+
+  // the page of keys 8 (r16 / 4) .. + 7 of a block (a page holds whole eights)
+  auto pages = [&](int j0) __attribute__((always_inline)) {
+    const int slot = j0 + 8 * (r16 >> 2);
+    return table[(slot < S ? slot : S - 1) >> b.page_shift];
+  };
+  constexpr int ROWS = 64 / PIECES;                        // 4 or 8 rows of V a load: within an eight
+  Frag kf[2][1][2][ES];
+  u32x4_t vr[LOADS];
+  auto load_k = [&](Frag (&kf)[1][2][ES], int j0, int id) __attribute__((always_inline)) {
+    const int held = (unsigned)id < (unsigned)b.n_pages ? id : 0;
+    const bf16_t* krow = kp + held * page_elems + (size_t)((j0 + 8 * (r16 >> 2) + (r16 & 3)) & in_page) * HD + g * 8;
+#pragma unroll
+    for (int bl = 0; bl < 2; ++bl)
+#pragma unroll
+      for (int es = 0; es < ES; ++es) kf[0][bl][es].nat = ((const Loose16*)(krow + bl * 4 * HD + es * 32))->v;
+  };
+  auto load_v = [&](int j0, int id) __attribute__((always_inline)) {
+    const int held = (unsigned)id < (unsigned)b.n_pages ? id : 0;
+#pragma unroll
+    for (int i = 0; i < LOADS; ++i) {
+      const int page = __builtin_amdgcn_readlane(held, i * ROWS / 8 * 4), row0 = (j0 + i * ROWS) & in_page;
+      vr[i] = ((const Loose16*)(vp + page * page_elems + (size_t)row0 * HD + lane * 8))->v;
+    }
+  };
+  auto store_v = [&](uint32_t there) __attribute__((always_inline)) {
+#pragma unroll
+    for (int i = 0; i < LOADS; ++i) {
+      const int row = i * ROWS + lane / PIECES, piece = lane % PIECES;
+      if (there != 0xffffffffu && !(there >> row & 1)) vr[i] = u32x4_t{0, 0, 0, 0};
+      *(u32x4_t*)(v_rows + row * (HD * 2) + v_place<HD>(row, piece >> 1) + (piece & 1) * 16) = vr[i];
+    }
+  };
+  // one block: its V goes to LDS, the next one's K and V are requested, then the products
+  auto block = [&](Frag (&now)[1][2][ES], Frag (&next)[1][2][ES], int j0, int id, int id_next) __attribute__((always_inline)) {
+    const uint64_t ok = __ballot((unsigned)id < (unsigned)b.n_pages);
+    uint32_t there = (ok & 1 ? 0xffu : 0u) | (ok & 0x10 ? 0xff00u : 0u) | (ok & 0x100 ? 0xff0000u : 0u) | (ok & 0x1000 ? 0xff000000u : 0u);
+    if (j0 + 32 > S) there &= (1u << (S - j0)) - 1;        // (j0 < S)
+    if (j0 + STEP < sl.key1) load_k(next, j0 + STEP, id_next);
+    store_v(there);
+    if (j0 + STEP < sl.key1) load_v(j0 + STEP, id_next);
+    auto k_of = [&](int, int bl, int es) __attribute__((always_inline)) { return now[0][bl][es]; };
+    uint64_t vis[QB];
+    if (there == 0xffffffffu && j0 + 32 <= sp.n) {
+      cols.template multiply<1, false>(k_of, v_rows, vis, a.scale_log2, r16, g);
+    } else {
+#pragma unroll
+      for (int qb = 0; qb < QB; ++qb) vis[qb] = cols.seen(a, sp, qb, j0, there);
+      cols.template multiply<1, true>(k_of, v_rows, vis, a.scale_log2, r16, g);
+    }
+  };
+  int j = sl.key0 + wave * 32;
+  if (j < sl.key1) {
+    int id0 = pages(j), id1 = pages(j + STEP);
+    load_k(kf[0], j, id0);
+    load_v(j, id0);
+    for (; j < sl.key1; j += 2 * STEP) {
+      const int id2 = pages(j + 2 * STEP), id3 = pages(j + 3 * STEP);
+      block(kf[0], kf[1], j, id0, id1);
+      if (j + STEP < sl.key1) block(kf[1], kf[0], j + STEP, id1, id2);
+      id0 = id2, id1 = id3;
+    }
+  }
+
+  // ---- join the wavefronts
+  const bool split_out = sl.count > 1;
+  float* po = split_out ? part_o + (size_t)split * b.rows * a.Hq * HD : nullptr;
+  float* pml = split_out ? part_ml + (size_t)split * b.rows * a.Hq * 2 : nullptr;
+  float* lds_o = (float*)lds;
+#pragma unroll
+  for (int qb = 0; qb < QB; ++qb) {
+    __syncthreads();
+    lds_m[wave * 64 + lane] = cols.m[qb];
+    lds_l[wave * 64 + lane] = sum_over_groups(cols.l[qb]);
+#pragma unroll
+    for (int eb = 0; eb < EB; ++eb) *(floatx4_t*)(lds_o + ((wave * EB + eb) * 64 + lane) * 4) = cols.o[qb][eb];
+    __syncthreads();
+    float top = -INFINITY, f[4], sum = 0.f;
+#pragma unroll
+    for (int w = 0; w < 4; ++w) top = fmaxf(top, lds_m[w * 64 + lane]);
+    const float ref = top == -INFINITY ? 0.f : top;
+#pragma unroll
+    for (int w = 0; w < 4; ++w) {
+      f[w] = __builtin_amdgcn_exp2f(lds_m[w * 64 + lane] - ref);
+      sum += f[w] * lds_l[w * 64 + lane];
+    }
+#pragma unroll
+    for (int eb = 0; eb < EB; eb += 4) {
+      if (eb + wave >= EB) continue;
+      floatx4_t acc = floatx4_t{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int w = 0; w < 4; ++w) {
+        const floatx4_t x = *(const floatx4_t*)(lds_o + ((w * EB + eb + wave) * 64 + lane) * 4);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) acc[i] = fmaf(f[w], x[i], acc[i]);
+      }
+      cols.finish(a, sp, qb, acc, eb + wave, sum, g, po);
+    }
+    if (split_out && wave == 0 && g == 0) cols.finish_sum(a, sp, qb, top, sum, pml);
+  }
+}
+
+// More columns: every wavefront owns QB blocks of 16, tiles of 64 keys of K and V go through LDS for all of them, two tiles in turn:
+// the next is on its way to registers while one is multiplied, and one barrier per tile is enough.
+template <int HD, int QB, int NW>
+__global__ __launch_bounds__(64 * NW, 2) void paged_attn_tile_kernel(PagedRows b, AttnRows a, int split_len, int col_tiles, float* part_o,
+                                                                    float* part_ml) {
+  using Cols = Columns<HD, QB>;
+  constexpr int ES = Cols::ES, EB = Cols::EB, PIECES = HD / 8, ROWS = 64 / PIECES, PASS = NW * ROWS, LOADS = 64 / PASS;
+  constexpr int TILE = 64 * HD * 2;
+  extern __shared__ __attribute__((aligned(1024))) unsigned char lds[];     // two stages of (K tile, V tile)
+  const int seq = blockIdx.z, hk = blockIdx.x, group = a.Hq / b.Hkv, split = blockIdx.y / col_tiles;
+  const int wg_col0 = (blockIdx.y % col_tiles) * (NW * QB * 16);
+  const SeqSpan sp = seq_span(b, seq);
+  const Slice sl = slice_of(sp, split, split_len);
+  if (wg_col0 >= sp.count * group || sl.key0 >= sl.key1) return;
+  const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, r16 = lane & 15, g = lane >> 4;
+  const int S = sp.n + sp.count, in_page = (1 << b.page_shift) - 1;
+  const size_t page_elems = (size_t)b.Hkv * HD << b.page_shift, head_elems = (size_t)hk * HD << b.page_shift;
+  const int32_t* table = b.table + (size_t)seq * b.table_width;
+  const bf16_t *kp = (const bf16_t*)a.k_pages + head_elems, *vp = (const bf16_t*)a.v_pages + head_elems;
+  const bool works = wg_col0 + wave * QB * 16 < sp.count * group;          // the others only bring tiles
+
+  Cols cols;
+  cols.start(a, sp, hk, group, wg_col0 + wave * QB * 16, r16, g);
+
+  u32x4_t kr[LOADS], vr[LOADS];
+  auto pages = [&](int j0) __attribute__((always_inline)) {                 // of key j0 + lane
+    const int slot = j0 + lane;
+    return table[(slot < S ? slot : S - 1) >> b.page_shift];
+  };
+  auto there_of = [&](int j0, int id) __attribute__((always_inline)) { return __ballot((unsigned)id < (unsigned)b.n_pages && j0 + lane < S); };
+  auto load = [&](int j0, int id) __attribute__((always_inline)) {
+    const int held = (unsigned)id < (unsigned)b.n_pages ? id : 0;
+#pragma unroll
+    for (int p = 0; p < LOADS; ++p) {
+      const int row0 = p * PASS + wave * ROWS;
+      const size_t at = __builtin_amdgcn_readlane(held, row0) * page_elems + (size_t)((j0 + row0) & in_page) * HD;
+      kr[p] = ((const Loose16*)(kp + at + lane * 8))->v;
+      vr[p] = ((const Loose16*)(vp + at + lane * 8))->v;
+    }
+  };
+  auto store = [&](int stage, uint64_t there) __attribute__((always_inline)) {
+    unsigned char* base = lds + stage * 2 * TILE;
+#pragma unroll
+    for (int p = 0; p < LOADS; ++p) {
+      const int row = p * PASS + wave * ROWS + lane / PIECES, piece = lane % PIECES;
+      if (there != ~0ull && !(there >> row & 1)) vr[p] = u32x4_t{0, 0, 0, 0};
+      *(u32x4_t*)(base + row * (HD * 2) + k_place<HD>(row, piece)) = kr[p];
+      *(u32x4_t*)(base + TILE + row * (HD * 2) + v_place<HD>(row, piece >> 1) + (piece & 1) * 16) = vr[p];
+    }
+  };
+
+  int id = pages(sl.key0);
+  uint64_t there = there_of(sl.key0, id);
+  load(sl.key0, id);
+  id = pages(sl.key0 + 64);
+  store(0, there);
+  __syncthreads();
+  int stage = 0;
+  for (int j0 = sl.key0; j0 < sl.key1; j0 += 64, stage ^= 1) {
+    const bool more = j0 + 64 < sl.key1;
+    const uint64_t there_next = there_of(j0 + 64, id);
+    if (more) {
+      load(j0 + 64, id);
+      id = pages(j0 + 128);
+    }
+    if (works) {
+      const unsigned char* base = lds + stage * 2 * TILE;
+      const int krow = 8 * (r16 >> 2) + (r16 & 3);
+      auto k_of = [&](int sub, int bl, int es) __attribute__((always_inline)) {
+        const int row = sub * 32 + 4 * bl + krow;
+        Frag f;
+        f.nat = *(const u32x4_t*)(base + row * (HD * 2) + k_place<HD>(row, es * 4 + g));
+        return f;
+      };
+      uint64_t vis[QB];
+      if (there == ~0ull && j0 + 64 <= sp.n) {
+        cols.template multiply<2, false>(k_of, base + TILE, vis, a.scale_log2, r16, g);
+      } else {
+#pragma unroll
+        for (int qb = 0; qb < QB; ++qb) vis[qb] = cols.seen(a, sp, qb, j0, there);
+        cols.template multiply<2, true>(k_of, base + TILE, vis, a.scale_log2, r16, g);
+      }
+    }
+    there = there_next;
+    if (more) store(stage ^ 1, there);
+    __syncthreads();
+  }
+
+  if (!works) return;
+  const bool split_out = sl.count > 1;
+  float* po = split_out ? part_o + (size_t)split * b.rows * a.Hq * HD : nullptr;
+  float* pml = split_out ? part_ml + (size_t)split * b.rows * a.Hq * 2 : nullptr;
+#pragma unroll
+  for (int qb = 0; qb < QB; ++qb) {
+    const float sum = sum_over_groups(cols.l[qb]);
+#pragma unroll
+    for (int eb = 0; eb < EB; ++eb) cols.finish(a, sp, qb, cols.o[qb][eb], eb, sum, g, po);
+    if (split_out && g == 0) cols.finish_sum(a, sp, qb, cols.m[qb], sum, pml);
+  }
+}
+
+// out = sum_s 2^(m_s - m) O_s / sum_s 2^(m_s - m) l_s over the slices of a sequence, in index order; four elements a thread
+template <int HD>
+__global__ __launch_bounds__(256) void paged_attn_join_kernel(PagedRows b, AttnRows a, int split_len, const float* part_o, const float* part_ml) {
+  const SeqSpan sp = seq_span(b, blockIdx.y);
+  const int count = slice_of(sp, 0, split_len).count;
+  const int at = blockIdx.x * 256 + threadIdx.x, e = at % (HD / 4) * 4, rh = at / (HD / 4), row = rh / a.Hq, head = rh % a.Hq;
+  if (count <= 1 || row >= sp.count) return;
+  const size_t rows = (size_t)b.rows * a.Hq, mine = (size_t)(sp.row0 + row) * a.Hq + head;
+  float top = -INFINITY;
+  for (int s = 0; s < count; ++s) top = fmaxf(top, part_ml[(s * rows + mine) * 2]);
+  const float ref = top == -INFINITY ? 0.f : top;
+  float sum = 0.f;
+  floatx4_t acc = floatx4_t{0.f, 0.f, 0.f, 0.f};
+#pragma unroll 4
+  for (int s = 0; s < count; ++s) {
+    const float2 ml = *(const float2*)(part_ml + (s * rows + mine) * 2);
+    const floatx4_t x = *(const floatx4_t*)(part_o + (s * rows + mine) * HD + e);
+    const float f = __builtin_amdgcn_exp2f(ml.x - ref);
+    sum = fmaf(f, ml.y, sum);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) acc[i] = fmaf(f, x[i], acc[i]);
+  }
+  const float inv = sum == 0.f ? 0.f : 1.0f / sum;
+  ((Loose8*)((bf16_t*)a.out + (int64_t)(sp.row0 + row) * a.out_stride + (int64_t)head * HD + e))->v =
+      sum == 0.f ? make_uint2(0, 0) : pack4_bf16(acc[0] * inv, acc[1] * inv, acc[2] * inv, acc[3] * inv);
+}
+
+namespace {
+// How a call runs: from its bounds alone, so that a captured call fits whatever its tables say later
+struct AttnPlan {
+  int blocks;                    // column blocks of 16 a wavefront owns
+  bool few, simple;
+  int col_tiles, split_len, splits;
+};
+AttnPlan attn_plan(int dtype, const PagedRows& b, int Hq) {
+  AttnPlan p{};
+  const int cols = b.max_rows * (Hq / b.Hkv), S = b.max_len + b.max_rows;
+  p.simple = dtype == 0 || (b.hd != 64 && b.hd != 128);
+  p.split_len = S, p.splits = 1;
+  if (p.simple) return p;
+  p.few = cols <= 32;
+  p.blocks = p.few ? (cols <= 16 ? 1 : 2) : cols <= 64 ? 1 : 2;
+  p.col_tiles = p.few ? 1 : (cols + 64 * p.blocks - 1) / (64 * p.blocks);
+  const int64_t groups = (int64_t)b.seqs * b.Hkv * p.col_tiles, want = p.few ? 1024 : 512;
+  const int least = p.few ? 256 : 512;
+  int64_t splits = (want + groups - 1) / groups;
+  if (splits > S / least) splits = S / least;
+  if (splits < 1) splits = 1;
+  p.split_len = (int)(((S + splits - 1) / splits + 63) / 64 * 64);
+  p.splits = (S + p.split_len - 1) / p.split_len;
+  return p;
+}
+template <int HD> hipError_t launch_attn_hd(const AttnPlan& p, const PagedRows& b, const AttnRows& a, float* part_o, float* part_ml, hipStream_t s) {
+  const dim3 grid(b.Hkv, p.splits * p.col_tiles, b.seqs);
+  if (p.few) {
+    auto f = p.blocks == 1 ? paged_attn_few_kernel<HD, 1> : paged_attn_few_kernel<HD, 2>;
+    hipLaunchKernelGGL(f, grid, dim3(256), 0, s, b, a, p.split_len, part_o, part_ml);
+  } else {
+    auto f = p.blocks == 1 ? paged_attn_tile_kernel<HD, 1, 4> : paged_attn_tile_kernel<HD, 2, 4>;
+    hipLaunchKernelGGL(f, grid, dim3(256), 4 * 64 * HD * 2, s, b, a, p.split_len, p.col_tiles, part_o, part_ml);
+  }
+  if (p.splits > 1) {
+    const int64_t threads = (int64_t)b.max_rows * a.Hq * (HD / 4);
+    hipLaunchKernelGGL(paged_attn_join_kernel<HD>, dim3((threads + 255) / 256, b.seqs), dim3(256), 0, s, b, a, p.split_len, part_o, part_ml);
+  }
   return hipGetLastError();
+}
+}  // namespace
+
+size_t paged_attn_scratch_bytes(int dtype, const PagedRows& b, int Hq) {
+  const AttnPlan p = attn_plan(dtype, b, Hq);
+  return p.splits > 1 ? (size_t)p.splits * b.rows * Hq * (b.hd + 2) * sizeof(float) : 0;
+}
+
+hipError_t launch_paged_attn(int dtype, const PagedRows& b, const AttnRows& a, void* scratch, hipStream_t s) {
+  const AttnPlan p = attn_plan(dtype, b, a.Hq);
+  if (p.simple) {
+    const dim3 grid(a.Hq, b.max_rows, b.seqs);
+    if (dtype == 0) hipLaunchKernelGGL(paged_attn_simple_kernel<float>, grid, dim3(64), 0, s, b, a);
+    else hipLaunchKernelGGL(paged_attn_simple_kernel<bf16_t>, grid, dim3(64), 0, s, b, a);
+    return hipGetLastError();
+  }
+  float* part_o = (float*)scratch;
+  float* part_ml = part_o + (size_t)p.splits * b.rows * a.Hq * b.hd;
+  return b.hd == 64 ? launch_attn_hd<64>(p, b, a, part_o, part_ml, s) : launch_attn_hd<128>(p, b, a, part_o, part_ml, s);
 }
 
 }  // namespace ht
