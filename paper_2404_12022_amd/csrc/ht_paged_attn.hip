@@ -5,6 +5,7 @@
 //
 // Slots whose page is none of the pool's are seen by nobody; a row that sees nothing is 0.
 #include "ht_common.h"
+#include <type_traits>
 
 namespace ht {
 
@@ -351,15 +352,15 @@ __global__ __launch_bounds__(256, 2) void paged_attn_few_kernel(PagedRows b, Att
     return table[(slot < S ? slot : S - 1) >> b.page_shift];
   };
   constexpr int ROWS = 64 / PIECES;                        // 4 or 8 rows of V a load: within an eight
-  Frag kf[2][1][2][ES];
+  Frag kf[2][ES];
   u32x4_t vr[LOADS];
-  auto load_k = [&](Frag (&kf)[1][2][ES], int j0, int id) __attribute__((always_inline)) {
+  auto load_k = [&](Frag (&to)[2][ES], int j0, int id) __attribute__((always_inline)) {
     const int held = (unsigned)id < (unsigned)b.n_pages ? id : 0;
     const bf16_t* krow = kp + held * page_elems + (size_t)((j0 + 8 * (r16 >> 2) + (r16 & 3)) & in_page) * HD + g * 8;
 #pragma unroll
     for (int bl = 0; bl < 2; ++bl)
 #pragma unroll
-      for (int es = 0; es < ES; ++es) kf[0][bl][es].nat = ((const Loose16*)(krow + bl * 4 * HD + es * 32))->v;
+      for (int es = 0; es < ES; ++es) to[bl][es].nat = ((const Loose16*)(krow + bl * 4 * HD + es * 32))->v;
   };
   auto load_v = [&](int j0, int id) __attribute__((always_inline)) {
     const int held = (unsigned)id < (unsigned)b.n_pages ? id : 0;
@@ -377,35 +378,45 @@ __global__ __launch_bounds__(256, 2) void paged_attn_few_kernel(PagedRows b, Att
       *(u32x4_t*)(v_rows + row * (HD * 2) + v_place<HD>(row, piece >> 1) + (piece & 1) * 16) = vr[i];
     }
   };
-  // one block: its V goes to LDS, the next one's K and V are requested, then the products
-  auto block = [&](Frag (&now)[1][2][ES], Frag (&next)[1][2][ES], int j0, int id, int id_next) __attribute__((always_inline)) {
+  auto there_of = [&](int j0, int id) __attribute__((always_inline)) {
     const uint64_t ok = __ballot((unsigned)id < (unsigned)b.n_pages);
-    uint32_t there = (ok & 1 ? 0xffu : 0u) | (ok & 0x10 ? 0xff00u : 0u) | (ok & 0x100 ? 0xff0000u : 0u) | (ok & 0x1000 ? 0xff000000u : 0u);
-    if (j0 + 32 > S) there &= (1u << (S - j0)) - 1;        // (j0 < S)
-    if (j0 + STEP < sl.key1) load_k(next, j0 + STEP, id_next);
-    store_v(there);
-    if (j0 + STEP < sl.key1) load_v(j0 + STEP, id_next);
-    auto k_of = [&](int, int bl, int es) __attribute__((always_inline)) { return now[0][bl][es]; };
-    uint64_t vis[QB];
-    if (there == 0xffffffffu && j0 + 32 <= sp.n) {
-      cols.template multiply<1, false>(k_of, v_rows, vis, a.scale_log2, r16, g);
-    } else {
-#pragma unroll
-      for (int qb = 0; qb < QB; ++qb) vis[qb] = cols.seen(a, sp, qb, j0, there);
-      cols.template multiply<1, true>(k_of, v_rows, vis, a.scale_log2, r16, g);
-    }
+    const uint32_t t = (ok & 1 ? 0xffu : 0u) | (ok & 0x10 ? 0xff00u : 0u) | (ok & 0x100 ? 0xff0000u : 0u) | (ok & 0x1000 ? 0xff000000u : 0u);
+    return j0 + 32 > S ? t & ((1u << (S - j0)) - 1) : t;   // (j0 < S)
   };
-  int j = sl.key0 + wave * 32;
-  if (j < sl.key1) {
-    int id0 = pages(j), id1 = pages(j + STEP);
-    load_k(kf[0], j, id0);
-    load_v(j, id0);
-    for (; j < sl.key1; j += 2 * STEP) {
-      const int id2 = pages(j + 2 * STEP), id3 = pages(j + 3 * STEP);
-      block(kf[0], kf[1], j, id0, id1);
-      if (j + STEP < sl.key1) block(kf[1], kf[0], j + STEP, id1, id2);
-      id0 = id2, id1 = id3;
-    }
+  int j0 = sl.key0 + wave * 32;
+  if (j0 < sl.key1) {
+    int id = pages(j0), id_next = pages(j0 + STEP);
+    load_k(kf, j0, id);
+    load_v(j0, id);
+    // a loop for the blocks that every column sees whole, and one for those behind (they hold rows of the pass; or a page is missing).
+    // A block: its V goes to LDS, the next one's K and V are requested, then the products
+    auto blocks = [&](auto masked) __attribute__((always_inline)) {
+      constexpr bool MASKED = decltype(masked)::value;
+      while (j0 < sl.key1) {
+        const uint32_t there = there_of(j0, id);
+        if (!MASKED && (there != 0xffffffffu || j0 + 32 > sp.n)) break;
+        const int id_after = pages(j0 + 2 * STEP);
+        const bool more = j0 + STEP < sl.key1;
+        Frag kn[2][ES];
+        if (more) load_k(kn, j0 + STEP, id_next);
+        store_v(MASKED ? there : 0xffffffffu);
+        if (more) load_v(j0 + STEP, id_next);
+        uint64_t vis[QB] = {};
+        if (MASKED) {
+#pragma unroll
+          for (int qb = 0; qb < QB; ++qb) vis[qb] = cols.seen(a, sp, qb, j0, there);
+        }
+        cols.template multiply<1, MASKED>([&](int, int bl, int es) __attribute__((always_inline)) { return kf[bl][es]; }, v_rows, vis,
+                                          a.scale_log2, r16, g);
+#pragma unroll
+        for (int bl = 0; bl < 2; ++bl)
+#pragma unroll
+          for (int es = 0; es < ES; ++es) kf[bl][es] = kn[bl][es];
+        id = id_next, id_next = id_after, j0 += STEP;
+      }
+    };
+    blocks(std::false_type{});
+    blocks(std::true_type{});
   }
 
   // ---- join the wavefronts
@@ -497,42 +508,46 @@ __global__ __launch_bounds__(64 * NW, 2) void paged_attn_tile_kernel(PagedRows b
     }
   };
 
-  int id = pages(sl.key0);
+  int id = pages(sl.key0), j0 = sl.key0, stage = 0;
   uint64_t there = there_of(sl.key0, id);
   load(sl.key0, id);
   id = pages(sl.key0 + 64);
   store(0, there);
   __syncthreads();
-  int stage = 0;
-  for (int j0 = sl.key0; j0 < sl.key1; j0 += 64, stage ^= 1) {
-    const bool more = j0 + 64 < sl.key1;
-    const uint64_t there_next = there_of(j0 + 64, id);
-    if (more) {
-      load(j0 + 64, id);
-      id = pages(j0 + 128);
-    }
-    if (works) {
-      const unsigned char* base = lds + stage * 2 * TILE;
-      const int krow = 8 * (r16 >> 2) + (r16 & 3);
-      auto k_of = [&](int sub, int bl, int es) __attribute__((always_inline)) {
-        const int row = sub * 32 + 4 * bl + krow;
-        Frag f;
-        f.nat = *(const u32x4_t*)(base + row * (HD * 2) + k_place<HD>(row, es * 4 + g));
-        return f;
-      };
-      uint64_t vis[QB];
-      if (there == ~0ull && j0 + 64 <= sp.n) {
-        cols.template multiply<2, false>(k_of, base + TILE, vis, a.scale_log2, r16, g);
-      } else {
-#pragma unroll
-        for (int qb = 0; qb < QB; ++qb) vis[qb] = cols.seen(a, sp, qb, j0, there);
-        cols.template multiply<2, true>(k_of, base + TILE, vis, a.scale_log2, r16, g);
+  // a loop for the tiles that every column sees whole, and one for those behind (they hold rows of the pass; or a page is missing)
+  auto tiles = [&](auto masked) __attribute__((always_inline)) {
+    constexpr bool MASKED = decltype(masked)::value;
+    for (; j0 < sl.key1; j0 += 64, stage ^= 1) {
+      if (!MASKED && (there != ~0ull || j0 + 64 > sp.n)) break;
+      const bool more = j0 + 64 < sl.key1;
+      const uint64_t there_next = there_of(j0 + 64, id);
+      if (more) {
+        load(j0 + 64, id);
+        id = pages(j0 + 128);
       }
+      if (works) {
+        const unsigned char* base = lds + stage * 2 * TILE;
+        const int krow = 8 * (r16 >> 2) + (r16 & 3);
+        auto k_of = [&](int sub, int bl, int es) __attribute__((always_inline)) {
+          const int row = sub * 32 + 4 * bl + krow;
+          Frag f;
+          f.nat = *(const u32x4_t*)(base + row * (HD * 2) + k_place<HD>(row, es * 4 + g));
+          return f;
+        };
+        uint64_t vis[QB] = {};
+        if (MASKED) {
+#pragma unroll
+          for (int qb = 0; qb < QB; ++qb) vis[qb] = cols.seen(a, sp, qb, j0, there);
+        }
+        cols.template multiply<2, MASKED>(k_of, base + TILE, vis, a.scale_log2, r16, g);
+      }
+      there = there_next;
+      if (more) store(stage ^ 1, there);
+      __syncthreads();
     }
-    there = there_next;
-    if (more) store(stage ^ 1, there);
-    __syncthreads();
-  }
+  };
+  tiles(std::false_type{});
+  tiles(std::true_type{});
 
   if (!works) return;
   const bool split_out = sl.count > 1;
@@ -547,27 +562,61 @@ __global__ __launch_bounds__(64 * NW, 2) void paged_attn_tile_kernel(PagedRows b
   }
 }
 
-// out = sum_s 2^(m_s - m) O_s / sum_s 2^(m_s - m) l_s over the slices of a sequence, in index order; four elements a thread
-template <int HD>
-__global__ __launch_bounds__(256) void paged_attn_join_kernel(PagedRows b, AttnRows a, int split_len, const float* part_o, const float* part_ml) {
-  const SeqSpan sp = seq_span(b, blockIdx.y);
-  const int count = slice_of(sp, 0, split_len).count;
-  const int at = blockIdx.x * 256 + threadIdx.x, e = at % (HD / 4) * 4, rh = at / (HD / 4), row = rh / a.Hq, head = rh % a.Hq;
+// out = sum_s 2^(m_s - m) O_s / sum_s 2^(m_s - m) l_s over the slices of a sequence, in a fixed order.  A workgroup per (row, head) and
+// up to PARTS groups of HD / 4 threads that take every PARTS-th slice, four elements a thread; their sums meet in LDS.
+template <int HD, int PARTS>
+__global__ __launch_bounds__(PARTS * (HD / 4)) void paged_attn_join_kernel(PagedRows b, AttnRows a, int split_len, const float* part_o,
+                                                                          const float* part_ml) {
+  constexpr int T = HD / 4;
+  const SeqSpan sp = seq_span(b, blockIdx.z);
+  const int count = slice_of(sp, 0, split_len).count, row = blockIdx.y, head = blockIdx.x;
   if (count <= 1 || row >= sp.count) return;
+  const int part = threadIdx.x / T, e = threadIdx.x % T * 4;
   const size_t rows = (size_t)b.rows * a.Hq, mine = (size_t)(sp.row0 + row) * a.Hq + head;
-  float top = -INFINITY;
-  for (int s = 0; s < count; ++s) top = fmaxf(top, part_ml[(s * rows + mine) * 2]);
-  const float ref = top == -INFINITY ? 0.f : top;
-  float sum = 0.f;
+  __shared__ float lds_o[PARTS][HD];
+  __shared__ float2 lds_ml[PARTS];
+  float top = -INFINITY, sum = 0.f;
   floatx4_t acc = floatx4_t{0.f, 0.f, 0.f, 0.f};
-#pragma unroll 4
-  for (int s = 0; s < count; ++s) {
-    const float2 ml = *(const float2*)(part_ml + (s * rows + mine) * 2);
-    const floatx4_t x = *(const floatx4_t*)(part_o + (s * rows + mine) * HD + e);
-    const float f = __builtin_amdgcn_exp2f(ml.x - ref);
-    sum = fmaf(f, ml.y, sum);
+  constexpr int NS = 4;                                    // slices requested at a time
+  for (int s0 = part; s0 < count; s0 += NS * PARTS) {
+    float2 ml[NS];
+    floatx4_t x[NS];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) acc[i] = fmaf(f, x[i], acc[i]);
+    for (int i = 0; i < NS; ++i) {
+      const int s = s0 + i * PARTS < count ? s0 + i * PARTS : s0;
+      ml[i] = *(const float2*)(part_ml + (s * rows + mine) * 2);
+      x[i] = *(const floatx4_t*)(part_o + (s * rows + mine) * HD + e);
+    }
+#pragma unroll
+    for (int i = 0; i < NS; ++i) {
+      if (s0 + i * PARTS >= count) break;
+      const float now = fmaxf(top, ml[i].x), ref = now == -INFINITY ? 0.f : now;
+      const float old = __builtin_amdgcn_exp2f(top - ref), f = __builtin_amdgcn_exp2f(ml[i].x - ref);
+      sum = fmaf(f, ml[i].y, sum * old);
+#pragma unroll
+      for (int c = 0; c < 4; ++c) acc[c] = fmaf(f, x[i][c], acc[c] * old);
+      top = now;
+    }
+  }
+  if constexpr (PARTS > 1) {
+    *(floatx4_t*)&lds_o[part][e] = acc;
+    if (e == 0) lds_ml[part] = make_float2(top, sum);
+    __syncthreads();
+    if (part) return;
+    float all = -INFINITY;
+#pragma unroll
+    for (int p = 0; p < PARTS; ++p) all = fmaxf(all, lds_ml[p].x);
+    const float ref = all == -INFINITY ? 0.f : all;
+    sum = 0.f;
+    acc = floatx4_t{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int p = 0; p < PARTS; ++p) {
+      const float f = __builtin_amdgcn_exp2f(lds_ml[p].x - ref);
+      sum = fmaf(f, lds_ml[p].y, sum);
+      const floatx4_t x = *(const floatx4_t*)&lds_o[p][e];
+#pragma unroll
+      for (int c = 0; c < 4; ++c) acc[c] = fmaf(f, x[c], acc[c]);
+    }
   }
   const float inv = sum == 0.f ? 0.f : 1.0f / sum;
   ((Loose8*)((bf16_t*)a.out + (int64_t)(sp.row0 + row) * a.out_stride + (int64_t)head * HD + e))->v =
@@ -609,8 +658,9 @@ template <int HD> hipError_t launch_attn_hd(const AttnPlan& p, const PagedRows& 
     hipLaunchKernelGGL(f, grid, dim3(256), 4 * 64 * HD * 2, s, b, a, p.split_len, p.col_tiles, part_o, part_ml);
   }
   if (p.splits > 1) {
-    const int64_t threads = (int64_t)b.max_rows * a.Hq * (HD / 4);
-    hipLaunchKernelGGL(paged_attn_join_kernel<HD>, dim3((threads + 255) / 256, b.seqs), dim3(256), 0, s, b, a, p.split_len, part_o, part_ml);
+    const dim3 rows(a.Hq, b.max_rows, b.seqs);
+    if (p.splits > 4) hipLaunchKernelGGL((paged_attn_join_kernel<HD, 8>), rows, dim3(8 * HD / 4), 0, s, b, a, p.split_len, part_o, part_ml);
+    else hipLaunchKernelGGL((paged_attn_join_kernel<HD, 1>), rows, dim3(HD / 4), 0, s, b, a, p.split_len, part_o, part_ml);
   }
   return hipGetLastError();
 }
