@@ -139,6 +139,116 @@ template <int HD> __device__ __forceinline__ Frag v_operand(const unsigned char*
   return f;
 }
 
+// Keys j0 .. j0 + 63 that row `row` of the sequence sees, as bits; `there`: those that are
+__device__ __forceinline__ uint64_t seen_bits(const AttnRows& a, const SeqSpan& sp, int row, int j0, uint64_t there) {
+  const int first = j0 - sp.n;                             // the row of the pass that key j0 is
+  if (first <= -64 || row >= sp.count) return there;
+  uint64_t bits;
+  if (!a.anc) {
+    const int upto = row - first;                          // rows 0 .. row
+    bits = upto < 0 ? 0ull : upto >= 63 ? ~0ull : (2ull << upto) - 1;
+  } else {
+    const uint64_t* w = a.anc + (size_t)(sp.row0 + row) * kMaskWords;
+    if (first < 0) {
+      bits = w[0] << -first | ((1ull << -first) - 1);
+    } else {
+      const int i = first >> 6, s = first & 63;
+      bits = i < kMaskWords ? w[i] >> s : 0ull;
+      if (s && i + 1 < kMaskWords) bits |= w[i + 1] << (64 - s);
+    }
+  }
+  return bits & there;
+}
+// Values that are no numbers become 0 (they would reach columns that do not see them); whether there were any
+__device__ __forceinline__ bool clear_odd(Frag& f) {
+  bool odd = false;
+#pragma unroll
+  for (int w = 0; w < 4; ++w) {
+    const bool lo = (f.u[w] & 0x7f80u) == 0x7f80u, hi = (f.u[w] & 0x7f800000u) == 0x7f800000u;
+    odd |= lo | hi;
+    f.u[w] &= (lo ? 0u : 0xffffu) | (hi ? 0u : 0xffff0000u);
+  }
+  return odd;
+}
+// The K place of the kernel with 32 columns to a wavefront, which reads 16 consecutive keys of one piece at a time
+template <int HD> __device__ __forceinline__ int wide_k_place(int row, int piece) {
+  return (piece ^ (HD == 128 ? row & 15 : (row >> 1) & 7)) << 4;
+}
+
+// Tiles of 64 keys for the NW wavefronts of a workgroup, through registers to two stages of (K, V) in LDS: the next tile is on its
+// way while one is multiplied, and one barrier per tile is enough.
+template <int HD, int NW, bool WIDE> struct TileLoader {
+  static constexpr int PIECES = HD / 8, ROWS = 64 / PIECES, PASS = NW * ROWS, LOADS = 64 / PASS, TILE = 64 * HD * 2;
+  const char *kp, *vp;
+  const int32_t* table;
+  size_t page_bytes;
+  int S, shift, n_pages, wave, lane;
+  u32x4_t kr[LOADS], vr[LOADS];
+
+  __device__ __forceinline__ TileLoader(const PagedRows& b, const AttnRows& a, const SeqSpan& sp, int seq, int hk, int wave, int lane)
+      : table(b.table + (size_t)seq * b.table_width), S(sp.n + sp.count), shift(b.page_shift), n_pages(b.n_pages), wave(wave), lane(lane) {
+    page_bytes = (size_t)b.Hkv * HD * 2 << shift;
+    const size_t head = (size_t)hk * HD * 2 << shift;
+    kp = (const char*)a.k_pages + head;
+    vp = (const char*)a.v_pages + head;
+  }
+  __device__ __forceinline__ int pages(int j0) const {      // of key j0 + lane
+    const int slot = j0 + lane;
+    return table[(slot < S ? slot : S - 1) >> shift];
+  }
+  __device__ __forceinline__ uint64_t there_of(int j0, int id) const { return __ballot((unsigned)id < (unsigned)n_pages && j0 + lane < S); }
+  __device__ __forceinline__ void load(int j0, int id) {
+    const int held = (unsigned)id < (unsigned)n_pages ? id : 0;
+#pragma unroll
+    for (int p = 0; p < LOADS; ++p) {                       // a load's rows lie in one page: pages hold whole eights
+      const int row0 = p * PASS + wave * ROWS;
+      const size_t at = __builtin_amdgcn_readlane(held, row0) * page_bytes + (size_t)((j0 + row0) & ((1 << shift) - 1)) * (HD * 2);
+      kr[p] = ((const Loose16*)(kp + at + (uint32_t)lane * 16u))->v;
+      vr[p] = ((const Loose16*)(vp + at + (uint32_t)lane * 16u))->v;
+    }
+  }
+  __device__ __forceinline__ void store(unsigned char* base, uint64_t there) {
+    if (there != ~0ull) {                                   // values of keys that are not there: 0 times what lies there is no 0
+#pragma unroll
+      for (int p = 0; p < LOADS; ++p)
+        if (!(there >> (p * PASS + wave * ROWS + lane / PIECES) & 1)) vr[p] = u32x4_t{0, 0, 0, 0};
+    }
+#pragma unroll
+    for (int p = 0; p < LOADS; ++p) {
+      const int row = p * PASS + wave * ROWS + lane / PIECES, piece = lane % PIECES;
+      *(u32x4_t*)(base + row * (HD * 2) + (WIDE ? wide_k_place<HD>(row, piece) : k_place<HD>(row, piece))) = kr[p];
+      *(u32x4_t*)(base + TILE + row * (HD * 2) + v_place<HD>(row, piece >> 1) + (piece & 1) * 16) = vr[p];
+    }
+  }
+  // A loop for the tiles that every column sees whole, and one for those behind (they hold rows of the pass; or a page is missing):
+  // f(masked, first key, keys that are there, tile)
+  template <typename F> __device__ __forceinline__ void run(unsigned char* lds, int key0, int key1, int n, F&& f) {
+    int id = pages(key0), j0 = key0, stage = 0;
+    uint64_t there = there_of(key0, id);
+    load(key0, id);
+    id = pages(key0 + 64);
+    store(lds, there);
+    __syncthreads();
+    auto tiles = [&](auto masked) __attribute__((always_inline)) {
+      for (; j0 < key1; j0 += 64, stage ^= 2 * TILE) {
+        if (!decltype(masked)::value && (there != ~0ull || j0 + 64 > n)) break;
+        const bool more = j0 + 64 < key1;
+        const uint64_t there_next = there_of(j0 + 64, id);
+        if (more) {
+          load(j0 + 64, id);
+          id = pages(j0 + 128);
+        }
+        f(masked, j0, there, (const unsigned char*)lds + stage);
+        there = there_next;
+        if (more) store(lds + (stage ^ 2 * TILE), there);
+        __syncthreads();
+      }
+    };
+    tiles(std::false_type{});
+    tiles(std::true_type{});
+  }
+};
+
 // Columns of a wavefront: QB blocks of 16
 template <int HD, int QB> struct Columns {
   static constexpr int ES = HD / 32, EB = HD / 16;
@@ -162,27 +272,6 @@ template <int HD, int QB> struct Columns {
 #pragma unroll
       for (int eb = 0; eb < EB; ++eb) o[qb][eb] = floatx4_t{0.f, 0.f, 0.f, 0.f};
     }
-  }
-
-  // Keys j0 .. j0 + 63 that column block qb sees, as bits; `there`: those that are
-  __device__ __forceinline__ uint64_t seen(const AttnRows& a, const SeqSpan& sp, int qb, int j0, uint64_t there) const {
-    const int first = j0 - sp.n;                           // the row of the pass that key j0 is
-    if (first <= -64 || row[qb] >= sp.count) return there;
-    uint64_t bits;
-    if (!a.anc) {
-      const int upto = row[qb] - first;                    // rows 0 .. row
-      bits = upto < 0 ? 0ull : upto >= 63 ? ~0ull : (2ull << upto) - 1;
-    } else {
-      const uint64_t* w = a.anc + (size_t)(sp.row0 + row[qb]) * kMaskWords;
-      if (first < 0) {
-        bits = w[0] << -first | ((1ull << -first) - 1);
-      } else {
-        const int i = first >> 6, s = first & 63;
-        bits = i < kMaskWords ? w[i] >> s : 0ull;
-        if (s && i + 1 < kMaskWords) bits |= w[i + 1] << (64 - s);
-      }
-    }
-    return bits & there;
   }
 
   // SUB blocks of 32 keys: k(sub, block, piece) their K operands, V rows in LDS, and with MASKED what every column sees of them
@@ -248,14 +337,7 @@ template <int HD, int QB> struct Columns {
 #pragma unroll
       for (int eb = 0; eb < EB; ++eb) {
         Frag vf = v_operand<HD>(rows, eb, r16, g);
-        if (MASKED) {                                      // a value that is no number would reach columns that do not see it
-#pragma unroll
-          for (int w = 0; w < 4; ++w) {
-            const bool lo = (vf.u[w] & 0x7f80u) == 0x7f80u, hi = (vf.u[w] & 0x7f800000u) == 0x7f800000u;
-            odd |= lo | hi;
-            vf.u[w] &= (lo ? 0u : 0xffffu) | (hi ? 0u : 0xffff0000u);
-          }
-        }
+        if (MASKED) odd |= clear_odd(vf);
 #pragma unroll
         for (int qb = 0; qb < QB; ++qb) o[qb][eb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf.v, pf[qb].v, o[qb][eb], 0, 0, 0);
       }
@@ -404,7 +486,7 @@ __global__ __launch_bounds__(256, 2) void paged_attn_few_kernel(PagedRows b, Att
         uint64_t vis[QB] = {};
         if (MASKED) {
 #pragma unroll
-          for (int qb = 0; qb < QB; ++qb) vis[qb] = cols.seen(a, sp, qb, j0, there);
+          for (int qb = 0; qb < QB; ++qb) vis[qb] = seen_bits(a, sp, cols.row[qb], j0, there);
         }
         cols.template multiply<1, MASKED>([&](int, int bl, int es) __attribute__((always_inline)) { return kf[bl][es]; }, v_rows, vis,
                                           a.scale_log2, r16, g);
@@ -457,14 +539,12 @@ __global__ __launch_bounds__(256, 2) void paged_attn_few_kernel(PagedRows b, Att
   }
 }
 
-// More columns: every wavefront owns QB blocks of 16, tiles of 64 keys of K and V go through LDS for all of them, two tiles in turn:
-// the next is on its way to registers while one is multiplied, and one barrier per tile is enough.
+// More columns: every wavefront owns QB blocks of 16, tiles of 64 keys of K and V go through LDS for all of them.
 template <int HD, int QB, int NW>
 __global__ __launch_bounds__(64 * NW, 2) void paged_attn_tile_kernel(PagedRows b, AttnRows a, int split_len, int col_tiles, float* part_o,
                                                                     float* part_ml) {
   using Cols = Columns<HD, QB>;
-  constexpr int ES = Cols::ES, EB = Cols::EB, PIECES = HD / 8, ROWS = 64 / PIECES, PASS = NW * ROWS, LOADS = 64 / PASS;
-  constexpr int TILE = 64 * HD * 2;
+  constexpr int EB = Cols::EB, TILE = 64 * HD * 2;
   extern __shared__ __attribute__((aligned(1024))) unsigned char lds[];     // two stages of (K tile, V tile)
   const int seq = blockIdx.z, hk = blockIdx.x, group = a.Hq / b.Hkv, split = blockIdx.y / col_tiles;
   const int wg_col0 = (blockIdx.y % col_tiles) * (NW * QB * 16);
@@ -472,82 +552,28 @@ __global__ __launch_bounds__(64 * NW, 2) void paged_attn_tile_kernel(PagedRows b
   const Slice sl = slice_of(sp, split, split_len);
   if (wg_col0 >= sp.count * group || sl.key0 >= sl.key1) return;
   const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, r16 = lane & 15, g = lane >> 4;
-  const int S = sp.n + sp.count, in_page = (1 << b.page_shift) - 1;
-  const size_t page_elems = (size_t)b.Hkv * HD << b.page_shift, head_elems = (size_t)hk * HD << b.page_shift;
-  const int32_t* table = b.table + (size_t)seq * b.table_width;
-  const bf16_t *kp = (const bf16_t*)a.k_pages + head_elems, *vp = (const bf16_t*)a.v_pages + head_elems;
   const bool works = wg_col0 + wave * QB * 16 < sp.count * group;          // the others only bring tiles
 
   Cols cols;
   cols.start(a, sp, hk, group, wg_col0 + wave * QB * 16, r16, g);
-
-  u32x4_t kr[LOADS], vr[LOADS];
-  auto pages = [&](int j0) __attribute__((always_inline)) {                 // of key j0 + lane
-    const int slot = j0 + lane;
-    return table[(slot < S ? slot : S - 1) >> b.page_shift];
-  };
-  auto there_of = [&](int j0, int id) __attribute__((always_inline)) { return __ballot((unsigned)id < (unsigned)b.n_pages && j0 + lane < S); };
-  auto load = [&](int j0, int id) __attribute__((always_inline)) {
-    const int held = (unsigned)id < (unsigned)b.n_pages ? id : 0;
-#pragma unroll
-    for (int p = 0; p < LOADS; ++p) {
-      const int row0 = p * PASS + wave * ROWS;
-      const size_t at = __builtin_amdgcn_readlane(held, row0) * page_elems + (size_t)((j0 + row0) & in_page) * HD;
-      kr[p] = ((const Loose16*)(kp + at + lane * 8))->v;
-      vr[p] = ((const Loose16*)(vp + at + lane * 8))->v;
-    }
-  };
-  auto store = [&](int stage, uint64_t there) __attribute__((always_inline)) {
-    unsigned char* base = lds + stage * 2 * TILE;
-#pragma unroll
-    for (int p = 0; p < LOADS; ++p) {
-      const int row = p * PASS + wave * ROWS + lane / PIECES, piece = lane % PIECES;
-      if (there != ~0ull && !(there >> row & 1)) vr[p] = u32x4_t{0, 0, 0, 0};
-      *(u32x4_t*)(base + row * (HD * 2) + k_place<HD>(row, piece)) = kr[p];
-      *(u32x4_t*)(base + TILE + row * (HD * 2) + v_place<HD>(row, piece >> 1) + (piece & 1) * 16) = vr[p];
-    }
-  };
-
-  int id = pages(sl.key0), j0 = sl.key0, stage = 0;
-  uint64_t there = there_of(sl.key0, id);
-  load(sl.key0, id);
-  id = pages(sl.key0 + 64);
-  store(0, there);
-  __syncthreads();
-  // a loop for the tiles that every column sees whole, and one for those behind (they hold rows of the pass; or a page is missing)
-  auto tiles = [&](auto masked) __attribute__((always_inline)) {
+  TileLoader<HD, NW, false> in(b, a, sp, seq, hk, wave, lane);
+  in.run(lds, sl.key0, sl.key1, sp.n, [&](auto masked, int j0, uint64_t there, const unsigned char* base) __attribute__((always_inline)) {
     constexpr bool MASKED = decltype(masked)::value;
-    for (; j0 < sl.key1; j0 += 64, stage ^= 1) {
-      if (!MASKED && (there != ~0ull || j0 + 64 > sp.n)) break;
-      const bool more = j0 + 64 < sl.key1;
-      const uint64_t there_next = there_of(j0 + 64, id);
-      if (more) {
-        load(j0 + 64, id);
-        id = pages(j0 + 128);
-      }
-      if (works) {
-        const unsigned char* base = lds + stage * 2 * TILE;
-        const int krow = 8 * (r16 >> 2) + (r16 & 3);
-        auto k_of = [&](int sub, int bl, int es) __attribute__((always_inline)) {
-          const int row = sub * 32 + 4 * bl + krow;
-          Frag f;
-          f.nat = *(const u32x4_t*)(base + row * (HD * 2) + k_place<HD>(row, es * 4 + g));
-          return f;
-        };
-        uint64_t vis[QB] = {};
-        if (MASKED) {
+    if (!works) return;
+    const int krow = 8 * (r16 >> 2) + (r16 & 3);
+    auto k_of = [&](int sub, int bl, int es) __attribute__((always_inline)) {
+      const int row = sub * 32 + 4 * bl + krow;
+      Frag f;
+      f.nat = *(const u32x4_t*)(base + row * (HD * 2) + k_place<HD>(row, es * 4 + g));
+      return f;
+    };
+    uint64_t vis[QB] = {};
+    if (MASKED) {
 #pragma unroll
-          for (int qb = 0; qb < QB; ++qb) vis[qb] = cols.seen(a, sp, qb, j0, there);
-        }
-        cols.template multiply<2, MASKED>(k_of, base + TILE, vis, a.scale_log2, r16, g);
-      }
-      there = there_next;
-      if (more) store(stage ^ 1, there);
-      __syncthreads();
+      for (int qb = 0; qb < QB; ++qb) vis[qb] = seen_bits(a, sp, cols.row[qb], j0, there);
     }
-  };
-  tiles(std::false_type{});
-  tiles(std::true_type{});
+    cols.template multiply<2, MASKED>(k_of, base + TILE, vis, a.scale_log2, r16, g);
+  });
 
   if (!works) return;
   const bool split_out = sl.count > 1;
@@ -559,6 +585,176 @@ __global__ __launch_bounds__(64 * NW, 2) void paged_attn_tile_kernel(PagedRows b
 #pragma unroll
     for (int eb = 0; eb < EB; ++eb) cols.finish(a, sp, qb, cols.o[qb][eb], eb, sum, g, po);
     if (split_out && g == 0) cols.finish_sum(a, sp, qb, cols.m[qb], sum, pml);
+  }
+}
+
+// Many columns: 32 to a wavefront, on the 32 x 32 x 16 instructions (half as many to issue, and a column lies in two lanes instead of
+// four).  Row r of a score product is key 16 (r / 16) + 8 (r / 4 % 2) + 4 (r / 8 % 2) + r % 4: the sixteen scores that a lane
+// holds of 32 keys are two runs of eight, P operands again.
+namespace {
+typedef float floatx16_t __attribute__((ext_vector_type(16)));
+
+template <int HD> struct WideColumns {
+  static constexpr int KS = HD / 16, EB = HD / 32;
+  Frag q[KS];
+  floatx16_t o[EB];
+  float m, l;
+  int row, head;
+
+  __device__ __forceinline__ void start(const AttnRows& a, const SeqSpan& sp, int hk, int group, int col, int half) {
+    row = col / group;
+    head = hk * group + col % group;
+    const int r = row < sp.count ? row : sp.count - 1;
+    const bf16_t* src = (const bf16_t*)a.q + (int64_t)(sp.row0 + r) * a.q_stride + (int64_t)head * HD + half * 8;
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks) q[ks].nat = ((const Loose16*)(src + ks * 16))->v;
+    m = -INFINITY;
+    l = 0.f;
+#pragma unroll
+    for (int eb = 0; eb < EB; ++eb)
+#pragma unroll
+      for (int x = 0; x < 16; ++x) o[eb][x] = 0.f;
+  }
+
+  template <bool MASKED>
+  __device__ __forceinline__ void multiply(const unsigned char* k_rows, const unsigned char* v_rows, uint64_t vis, float scale, int lane) {
+    const int r32 = lane & 31, half = lane >> 5, r16 = lane & 15;
+    const int krow = 16 * (r32 >> 4) + 8 * ((r32 >> 2) & 1) + 4 * ((r32 >> 3) & 1) + (r32 & 3);
+    float p[2][16];
+#pragma unroll
+    for (int kb = 0; kb < 2; ++kb) {
+      floatx16_t s;
+#pragma unroll
+      for (int x = 0; x < 16; ++x) s[x] = 0.f;
+#pragma unroll
+      for (int ks = 0; ks < KS; ++ks) {
+        Frag kf;
+        kf.nat = *(const u32x4_t*)(k_rows + (kb * 32 + krow) * (HD * 2) + wide_k_place<HD>(krow, 2 * ks + half));
+        s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf.v, q[ks].v, s, 0, 0, 0);
+      }
+#pragma unroll
+      for (int x = 0; x < 16; ++x) p[kb][x] = s[x];
+    }
+    if (MASKED) {
+#pragma unroll
+      for (int kb = 0; kb < 2; ++kb) {
+        const uint32_t word = (uint32_t)(vis >> kb * 32) >> half * 8;
+#pragma unroll
+        for (int x = 0; x < 16; ++x) p[kb][x] = word >> (16 * (x >> 3) + (x & 7)) & 1 ? p[kb][x] : -INFINITY;
+      }
+    }
+    float top = p[0][0];
+#pragma unroll
+    for (int x = 1; x < 32; ++x) top = fmaxf(top, p[x >> 4][x & 15]);
+    auto sw = __builtin_amdgcn_permlane32_swap(__float_as_uint(top), __float_as_uint(top), false, false);
+    top = fmaxf(__uint_as_float(sw[0]), __uint_as_float(sw[1])) * scale;
+    const bool grow = top > m + kRescaleStep;
+    if (__any(grow)) {
+      const float keep = grow ? __builtin_amdgcn_exp2f(m - top) : 1.0f;
+      l *= keep;
+#pragma unroll
+      for (int eb = 0; eb < EB; ++eb) o[eb] *= keep;
+      m = grow ? top : m;
+    }
+    const float ref = m == -INFINITY ? 0.f : m;
+#pragma unroll
+    for (int x = 0; x < 32; ++x) {
+      p[x >> 4][x & 15] = __builtin_amdgcn_exp2f(fmaf(p[x >> 4][x & 15], scale, -ref));
+      l += p[x >> 4][x & 15];
+    }
+#pragma unroll
+    for (int t = 0; t < 4; ++t) {                          // 16 keys
+      Frag pf;
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        const float* w = &p[t >> 1][8 * (t & 1) + 4 * h];
+        pf.half[h] = pack4_bf16(w[0], w[1], w[2], w[3]);
+      }
+      bool odd = false;
+#pragma unroll
+      for (int eb = 0; eb < EB; ++eb) {
+        Frag vf;
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          const int row = 8 * half + 4 * h + (r16 >> 2);
+          const unsigned char* at = v_rows + (16 * t + row) * (HD * 2) + v_place<HD>(row, eb * 2 + ((lane >> 4) & 1)) + (r16 & 3) * 8;
+          const s16x4_t x = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4_t*)at);
+          vf.half[h] = *(const uint2*)&x;
+        }
+        if (MASKED) odd |= clear_odd(vf);
+        o[eb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf.v, pf.v, o[eb], 0, 0, 0);
+      }
+      if (MASKED && __any(odd)) {                          // the values that are no numbers, to the columns that see them
+#pragma unroll 1
+        for (int key = 0; key < 16; ++key) {
+          float w = 0.f;
+#pragma unroll
+          for (int x = 0; x < 8; ++x) w = (key & 7) == x ? p[t >> 1][8 * (t & 1) + x] : w;
+          w = __shfl(w, (key >> 3) * 32 + r32, 64);
+#pragma unroll
+          for (int eb = 0; eb < EB; ++eb)
+#pragma unroll
+            for (int a4 = 0; a4 < 4; ++a4) {               // e = eb * 32 + 8 a4 + 4 half + i
+              const int unit = eb * 2 + (a4 >> 1);
+              const uint2 four = *(const uint2*)(v_rows + (16 * t + key) * (HD * 2) + v_place<HD>(key, unit) + (a4 & 1) * 16 + half * 8);
+#pragma unroll
+              for (int i = 0; i < 4; ++i) {
+                const uint32_t v = (i < 2 ? four.x : four.y) >> (i & 1) * 16 & 0xffffu;
+                if ((v & 0x7f80u) == 0x7f80u && w != 0.f) o[eb][a4 * 4 + i] += w * __uint_as_float(v << 16);
+              }
+            }
+        }
+      }
+    }
+  }
+};
+}  // namespace
+
+template <int HD, int NW>
+__global__ __launch_bounds__(64 * NW, 2) void paged_attn_wide_kernel(PagedRows b, AttnRows a, int split_len, int col_tiles, float* part_o,
+                                                                    float* part_ml) {
+  using Cols = WideColumns<HD>;
+  constexpr int EB = Cols::EB, TILE = 64 * HD * 2;
+  extern __shared__ __attribute__((aligned(1024))) unsigned char lds[];     // two stages of (K tile, V tile)
+  const int seq = blockIdx.z, hk = blockIdx.x, group = a.Hq / b.Hkv, split = blockIdx.y / col_tiles;
+  const int wg_col0 = (blockIdx.y % col_tiles) * (NW * 32);
+  const SeqSpan sp = seq_span(b, seq);
+  const Slice sl = slice_of(sp, split, split_len);
+  if (wg_col0 >= sp.count * group || sl.key0 >= sl.key1) return;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, half = lane >> 5;
+  const bool works = wg_col0 + wave * 32 < sp.count * group;                // the others only bring tiles
+  Cols cols;
+  cols.start(a, sp, hk, group, wg_col0 + wave * 32 + (lane & 31), half);
+  TileLoader<HD, NW, true> in(b, a, sp, seq, hk, wave, lane);
+  in.run(lds, sl.key0, sl.key1, sp.n, [&](auto masked, int j0, uint64_t there, const unsigned char* base) __attribute__((always_inline)) {
+    constexpr bool MASKED = decltype(masked)::value;
+    if (!works) return;
+    const uint64_t vis = MASKED ? seen_bits(a, sp, cols.row, j0, there) : 0ull;
+    cols.template multiply<MASKED>(base, base + TILE, vis, a.scale_log2, lane);
+  });
+  if (!works) return;
+  auto sw = __builtin_amdgcn_permlane32_swap(__float_as_uint(cols.l), __float_as_uint(cols.l), false, false);
+  const float sum = __uint_as_float(sw[0]) + __uint_as_float(sw[1]);
+  if (cols.row >= sp.count) return;
+  const int64_t at = sp.row0 + cols.row;
+  if (sl.count > 1) {
+    const size_t rows = (size_t)b.rows * a.Hq;
+    float* po = part_o + (split * rows + at * a.Hq + cols.head) * HD + half * 4;
+#pragma unroll
+    for (int eb = 0; eb < EB; ++eb)
+#pragma unroll
+      for (int a4 = 0; a4 < 4; ++a4)
+        *(float4*)(po + eb * 32 + a4 * 8) = make_float4(cols.o[eb][a4 * 4], cols.o[eb][a4 * 4 + 1], cols.o[eb][a4 * 4 + 2], cols.o[eb][a4 * 4 + 3]);
+    if (half == 0) *(float2*)(part_ml + (split * rows + at * a.Hq + cols.head) * 2) = make_float2(cols.m, sum);
+  } else {
+    const float inv = sum == 0.f ? 0.f : 1.0f / sum;
+    bf16_t* out = (bf16_t*)a.out + at * a.out_stride + (int64_t)cols.head * HD + half * 4;
+#pragma unroll
+    for (int eb = 0; eb < EB; ++eb)
+#pragma unroll
+      for (int a4 = 0; a4 < 4; ++a4)
+        ((Loose8*)(out + eb * 32 + a4 * 8))->v = sum == 0.f ? make_uint2(0, 0) :
+            pack4_bf16(cols.o[eb][a4 * 4] * inv, cols.o[eb][a4 * 4 + 1] * inv, cols.o[eb][a4 * 4 + 2] * inv, cols.o[eb][a4 * 4 + 3] * inv);
   }
 }
 
@@ -654,7 +850,7 @@ template <int HD> hipError_t launch_attn_hd(const AttnPlan& p, const PagedRows& 
     auto f = p.blocks == 1 ? paged_attn_few_kernel<HD, 1> : paged_attn_few_kernel<HD, 2>;
     hipLaunchKernelGGL(f, grid, dim3(256), 0, s, b, a, p.split_len, part_o, part_ml);
   } else {
-    auto f = p.blocks == 1 ? paged_attn_tile_kernel<HD, 1, 4> : paged_attn_tile_kernel<HD, 2, 4>;
+    auto f = p.blocks == 1 ? paged_attn_tile_kernel<HD, 1, 4> : paged_attn_wide_kernel<HD, 4>;
     hipLaunchKernelGGL(f, grid, dim3(256), 4 * 64 * HD * 2, s, b, a, p.split_len, p.col_tiles, part_o, part_ml);
   }
   if (p.splits > 1) {
