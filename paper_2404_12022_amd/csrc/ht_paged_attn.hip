@@ -175,15 +175,15 @@ template <int HD> __device__ __forceinline__ int wide_k_place(int row, int piece
   return (piece ^ (HD == 128 ? row & 15 : (row >> 1) & 7)) << 4;
 }
 
-// Tiles of 64 keys for the NW wavefronts of a workgroup, through registers to two stages of (K, V) in LDS: the next tile is on its
-// way while one is multiplied, and one barrier per tile is enough.
+// What a workgroup's NW wavefronts bring of a sequence's pages: tiles of 64 keys of K and V, through registers to LDS
 template <int HD, int NW, bool WIDE> struct TileLoader {
   static constexpr int PIECES = HD / 8, ROWS = 64 / PIECES, PASS = NW * ROWS, LOADS = 64 / PASS, TILE = 64 * HD * 2;
+  static_assert(64 % PASS == 0, "whole passes");
+  typedef u32x4_t Part[LOADS];                              // a wavefront's part of a tile
   const char *kp, *vp;
   const int32_t* table;
   size_t page_bytes;
   int S, shift, n_pages, wave, lane;
-  u32x4_t kr[LOADS], vr[LOADS];
 
   __device__ __forceinline__ TileLoader(const PagedRows& b, const AttnRows& a, const SeqSpan& sp, int seq, int hk, int wave, int lane)
       : table(b.table + (size_t)seq * b.table_width), S(sp.n + sp.count), shift(b.page_shift), n_pages(b.n_pages), wave(wave), lane(lane) {
@@ -197,35 +197,61 @@ template <int HD, int NW, bool WIDE> struct TileLoader {
     return table[(slot < S ? slot : S - 1) >> shift];
   }
   __device__ __forceinline__ uint64_t there_of(int j0, int id) const { return __ballot((unsigned)id < (unsigned)n_pages && j0 + lane < S); }
-  __device__ __forceinline__ void load(int j0, int id) {
+  __device__ __forceinline__ void load(Part& x, const char* pool, int j0, int id) const {
     const int held = (unsigned)id < (unsigned)n_pages ? id : 0;
 #pragma unroll
     for (int p = 0; p < LOADS; ++p) {                       // a load's rows lie in one page: pages hold whole eights
       const int row0 = p * PASS + wave * ROWS;
       const size_t at = __builtin_amdgcn_readlane(held, row0) * page_bytes + (size_t)((j0 + row0) & ((1 << shift) - 1)) * (HD * 2);
-      kr[p] = ((const Loose16*)(kp + at + (uint32_t)lane * 16u))->v;
-      vr[p] = ((const Loose16*)(vp + at + (uint32_t)lane * 16u))->v;
+      x[p] = ((const Loose16*)(pool + at + (uint32_t)lane * 16u))->v;
     }
   }
-  __device__ __forceinline__ void store(unsigned char* base, uint64_t there) {
-    if (there != ~0ull) {                                   // values of keys that are not there: 0 times what lies there is no 0
+  // The same with the pages of the wavefront's rows in scalar registers
+  __device__ __forceinline__ int page_at(int slot) const {
+    const auto* in = (const __attribute__((address_space(4))) int32_t*)(uintptr_t)table;
+    return in[(slot < S ? slot : S - 1) >> shift];
+  }
+  __device__ __forceinline__ void load(Part& x, const char* pool, int j0, const int (&id)[LOADS]) const {
 #pragma unroll
-      for (int p = 0; p < LOADS; ++p)
-        if (!(there >> (p * PASS + wave * ROWS + lane / PIECES) & 1)) vr[p] = u32x4_t{0, 0, 0, 0};
+    for (int p = 0; p < LOADS; ++p) {
+      const int row0 = p * PASS + wave * ROWS, held = (unsigned)id[p] < (unsigned)n_pages ? id[p] : 0;
+      const size_t at = held * page_bytes + (size_t)((j0 + row0) & ((1 << shift) - 1)) * (HD * 2);
+      x[p] = ((const Loose16*)(pool + at + (uint32_t)lane * 16u))->v;
     }
+  }
+  __device__ __forceinline__ void store_k(const Part& x, unsigned char* base) const {
 #pragma unroll
     for (int p = 0; p < LOADS; ++p) {
       const int row = p * PASS + wave * ROWS + lane / PIECES, piece = lane % PIECES;
-      *(u32x4_t*)(base + row * (HD * 2) + (WIDE ? wide_k_place<HD>(row, piece) : k_place<HD>(row, piece))) = kr[p];
-      *(u32x4_t*)(base + TILE + row * (HD * 2) + v_place<HD>(row, piece >> 1) + (piece & 1) * 16) = vr[p];
+      *(u32x4_t*)(base + row * (HD * 2) + (WIDE ? wide_k_place<HD>(row, piece) : k_place<HD>(row, piece))) = x[p];
     }
   }
-  // A loop for the tiles that every column sees whole, and one for those behind (they hold rows of the pass; or a page is missing):
+  __device__ __forceinline__ void store_v(const Part& x, unsigned char* base) const {
+#pragma unroll
+    for (int p = 0; p < LOADS; ++p) {
+      const int row = p * PASS + wave * ROWS + lane / PIECES, piece = lane % PIECES;
+      *(u32x4_t*)(base + row * (HD * 2) + v_place<HD>(row, piece >> 1) + (piece & 1) * 16) = x[p];
+    }
+  }
+  __device__ __forceinline__ void clear(Part& x, uint64_t there) const {  // values of keys that are not there: 0 times what lies there is no 0
+#pragma unroll
+    for (int p = 0; p < LOADS; ++p)
+      if (!(there >> (p * PASS + wave * ROWS + lane / PIECES) & 1)) x[p] = u32x4_t{0, 0, 0, 0};
+  }
+  // Tile after tile, the next on its way while one is multiplied, two stages of (K, V), a barrier per tile; a loop for the tiles that
+  // every column sees whole, and one for those behind (they hold rows of the pass; or a page is missing):
   // f(masked, first key, keys that are there, tile)
-  template <typename F> __device__ __forceinline__ void run(unsigned char* lds, int key0, int key1, int n, F&& f) {
+  template <typename F> __device__ __forceinline__ void run(unsigned char* lds, int key0, int key1, int n, F&& f) const {
+    Part k, v;
+    auto store = [&](unsigned char* base, uint64_t there) __attribute__((always_inline)) {
+      if (there != ~0ull) clear(v, there);
+      store_k(k, base);
+      store_v(v, base + TILE);
+    };
     int id = pages(key0), j0 = key0, stage = 0;
     uint64_t there = there_of(key0, id);
-    load(key0, id);
+    load(k, kp, key0, id);
+    load(v, vp, key0, id);
     id = pages(key0 + 64);
     store(lds, there);
     __syncthreads();
@@ -235,7 +261,8 @@ template <int HD, int NW, bool WIDE> struct TileLoader {
         const bool more = j0 + 64 < key1;
         const uint64_t there_next = there_of(j0 + 64, id);
         if (more) {
-          load(j0 + 64, id);
+          load(k, kp, j0 + 64, id);
+          load(v, vp, j0 + 64, id);
           id = pages(j0 + 128);
         }
         f(masked, j0, there, (const unsigned char*)lds + stage);
@@ -556,7 +583,7 @@ __global__ __launch_bounds__(64 * NW, 2) void paged_attn_tile_kernel(PagedRows b
 
   Cols cols;
   cols.start(a, sp, hk, group, wg_col0 + wave * QB * 16, r16, g);
-  TileLoader<HD, NW, false> in(b, a, sp, seq, hk, wave, lane);
+  const TileLoader<HD, NW, false> in(b, a, sp, seq, hk, wave, lane);
   in.run(lds, sl.key0, sl.key1, sp.n, [&](auto masked, int j0, uint64_t there, const unsigned char* base) __attribute__((always_inline)) {
     constexpr bool MASKED = decltype(masked)::value;
     if (!works) return;
@@ -616,28 +643,35 @@ template <int HD> struct WideColumns {
       for (int x = 0; x < 16; ++x) o[eb][x] = 0.f;
   }
 
-  template <bool MASKED>
-  __device__ __forceinline__ void multiply(const unsigned char* k_rows, const unsigned char* v_rows, uint64_t vis, float scale, int lane) {
-    const int r32 = lane & 31, half = lane >> 5, r16 = lane & 15;
+  // Scores of NB blocks of 32 keys
+  template <int NB> __device__ __forceinline__ void scores(const unsigned char* k_rows, float (&p)[NB][16], int lane) const {
+    const int r32 = lane & 31, half = lane >> 5;
     const int krow = 16 * (r32 >> 4) + 8 * ((r32 >> 2) & 1) + 4 * ((r32 >> 3) & 1) + (r32 & 3);
-    float p[2][16];
+    floatx16_t s[NB];
 #pragma unroll
-    for (int kb = 0; kb < 2; ++kb) {
-      floatx16_t s;
+    for (int kb = 0; kb < NB; ++kb)
 #pragma unroll
-      for (int x = 0; x < 16; ++x) s[x] = 0.f;
+      for (int x = 0; x < 16; ++x) s[kb][x] = 0.f;
 #pragma unroll
-      for (int ks = 0; ks < KS; ++ks) {
+    for (int ks = 0; ks < KS; ++ks)
+#pragma unroll
+      for (int kb = 0; kb < NB; ++kb) {
         Frag kf;
         kf.nat = *(const u32x4_t*)(k_rows + (kb * 32 + krow) * (HD * 2) + wide_k_place<HD>(krow, 2 * ks + half));
-        s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf.v, q[ks].v, s, 0, 0, 0);
+        s[kb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf.v, q[ks].v, s[kb], 0, 0, 0);
       }
 #pragma unroll
-      for (int x = 0; x < 16; ++x) p[kb][x] = s[x];
-    }
+    for (int kb = 0; kb < NB; ++kb)
+#pragma unroll
+      for (int x = 0; x < 16; ++x) p[kb][x] = s[kb][x];
+  }
+  // Their probabilities; the accumulators follow the reference point
+  template <bool MASKED, int NB>
+  __device__ __forceinline__ void soften(float (&p)[NB][16], Frag (&pf)[2 * NB], uint64_t vis, float scale, int lane) {
+    const int half = lane >> 5;
     if (MASKED) {
 #pragma unroll
-      for (int kb = 0; kb < 2; ++kb) {
+      for (int kb = 0; kb < NB; ++kb) {
         const uint32_t word = (uint32_t)(vis >> kb * 32) >> half * 8;
 #pragma unroll
         for (int x = 0; x < 16; ++x) p[kb][x] = word >> (16 * (x >> 3) + (x & 7)) & 1 ? p[kb][x] : -INFINITY;
@@ -645,7 +679,7 @@ template <int HD> struct WideColumns {
     }
     float top = p[0][0];
 #pragma unroll
-    for (int x = 1; x < 32; ++x) top = fmaxf(top, p[x >> 4][x & 15]);
+    for (int x = 1; x < 16 * NB; ++x) top = fmaxf(top, p[x >> 4][x & 15]);
     auto sw = __builtin_amdgcn_permlane32_swap(__float_as_uint(top), __float_as_uint(top), false, false);
     top = fmaxf(__uint_as_float(sw[0]), __uint_as_float(sw[1])) * scale;
     const bool grow = top > m + kRescaleStep;
@@ -658,18 +692,73 @@ template <int HD> struct WideColumns {
     }
     const float ref = m == -INFINITY ? 0.f : m;
 #pragma unroll
-    for (int x = 0; x < 32; ++x) {
-      p[x >> 4][x & 15] = __builtin_amdgcn_exp2f(fmaf(p[x >> 4][x & 15], scale, -ref));
-      l += p[x >> 4][x & 15];
-    }
+    for (int t = 0; t < 2 * NB; ++t) {
+      float w[8];
 #pragma unroll
-    for (int t = 0; t < 4; ++t) {                          // 16 keys
-      Frag pf;
+      for (int x = 0; x < 8; ++x) {
+        w[x] = __builtin_amdgcn_exp2f(fmaf(p[t >> 1][8 * (t & 1) + x], scale, -ref));
+        l += w[x];
+      }
+      pf[t].half[0] = pack4_bf16(w[0], w[1], w[2], w[3]);
+      pf[t].half[1] = pack4_bf16(w[4], w[5], w[6], w[7]);
+    }
+  }
+  // Operand of step i: in turn of the values (V^T, 32 columns e of 16 keys) and of the scores (K, 16 columns e of 32 keys)
+  template <int NB> __device__ __forceinline__ Frag operand(const unsigned char* v_rows, const unsigned char* k_rows, int i, int lane) const {
+    const int r32 = lane & 31, half = lane >> 5, r16 = lane & 15, n = i >> 1;
+    Frag f;
+    if (i & 1) {
+      const int krow = 16 * (r32 >> 4) + 8 * ((r32 >> 2) & 1) + 4 * ((r32 >> 3) & 1) + (r32 & 3), kb = n % NB, ks = n / NB;
+      f.nat = *(const u32x4_t*)(k_rows + (kb * 32 + krow) * (HD * 2) + wide_k_place<HD>(krow, 2 * ks + half));
+    } else {
+      const int eb = n % EB, t = n / EB;
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
-        const float* w = &p[t >> 1][8 * (t & 1) + 4 * h];
-        pf.half[h] = pack4_bf16(w[0], w[1], w[2], w[3]);
+        const int row = 8 * half + 4 * h + (r16 >> 2);
+        const unsigned char* at = v_rows + (16 * t + row) * (HD * 2) + v_place<HD>(row, eb * 2 + ((lane >> 4) & 1)) + (r16 & 3) * 8;
+        const s16x4_t x = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4_t*)at);
+        f.half[h] = *(const uint2*)&x;
       }
+    }
+    return f;
+  }
+  // The values of one tile and the scores of the next, step by step in turn (independent sums between dependent ones), the operands of
+  // AHEAD steps on their way from LDS: left to itself the compiler asks for two and waits for them
+  template <int NB>
+  __device__ __forceinline__ void advance(const unsigned char* v_rows, const unsigned char* k_rows, const Frag (&pf)[2 * NB], float (&p)[NB][16],
+                                          int lane) {
+    constexpr int STEPS = 2 * KS * NB, AHEAD = 6;
+    floatx16_t s[NB];
+#pragma unroll
+    for (int kb = 0; kb < NB; ++kb)
+#pragma unroll
+      for (int x = 0; x < 16; ++x) s[kb][x] = 0.f;
+    Frag ring[AHEAD];
+#pragma unroll
+    for (int i = 0; i < AHEAD; ++i) ring[i] = operand<NB>(v_rows, k_rows, i, lane);
+    __builtin_amdgcn_sched_group_barrier(0x100, AHEAD / 2 * 3, 0);          // LDS reads
+#pragma unroll
+    for (int i = 0; i < STEPS; ++i) {
+      const int n = i >> 1;
+      if (i & 1) s[n % NB] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(ring[i % AHEAD].v, q[n / NB].v, s[n % NB], 0, 0, 0);
+      else o[n % EB] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(ring[i % AHEAD].v, pf[n / EB].v, o[n % EB], 0, 0, 0);
+      if (i + AHEAD < STEPS) ring[i % AHEAD] = operand<NB>(v_rows, k_rows, i + AHEAD, lane);
+      __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);                    // a matrix instruction
+      if (i + AHEAD < STEPS) {
+        if (i & 1) __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+        else __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);
+      }
+    }
+#pragma unroll
+    for (int kb = 0; kb < NB; ++kb)
+#pragma unroll
+      for (int x = 0; x < 16; ++x) p[kb][x] = s[kb][x];
+  }
+  // Their values
+  template <bool MASKED, int NB> __device__ __forceinline__ void values(const unsigned char* v_rows, const Frag (&pf)[2 * NB], int lane) {
+    const int r32 = lane & 31, half = lane >> 5, r16 = lane & 15;
+#pragma unroll
+    for (int t = 0; t < 2 * NB; ++t) {                     // 16 keys
       bool odd = false;
 #pragma unroll
       for (int eb = 0; eb < EB; ++eb) {
@@ -682,15 +771,15 @@ template <int HD> struct WideColumns {
           vf.half[h] = *(const uint2*)&x;
         }
         if (MASKED) odd |= clear_odd(vf);
-        o[eb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf.v, pf.v, o[eb], 0, 0, 0);
+        o[eb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf.v, pf[t].v, o[eb], 0, 0, 0);
       }
       if (MASKED && __any(odd)) {                          // the values that are no numbers, to the columns that see them
 #pragma unroll 1
         for (int key = 0; key < 16; ++key) {
-          float w = 0.f;
+          uint32_t two = 0;
 #pragma unroll
-          for (int x = 0; x < 8; ++x) w = (key & 7) == x ? p[t >> 1][8 * (t & 1) + x] : w;
-          w = __shfl(w, (key >> 3) * 32 + r32, 64);
+          for (int x = 0; x < 4; ++x) two = (key >> 1 & 3) == x ? pf[t].u[x] : two;
+          const float w = __shfl(__uint_as_float(key & 1 ? two & 0xffff0000u : two << 16), (key >> 3) * 32 + r32, 64);
 #pragma unroll
           for (int eb = 0; eb < EB; ++eb)
 #pragma unroll
@@ -710,32 +799,152 @@ template <int HD> struct WideColumns {
 };
 }  // namespace
 
-template <int HD, int NW>
-__global__ __launch_bounds__(64 * NW, 2) void paged_attn_wide_kernel(PagedRows b, AttnRows a, int split_len, int col_tiles, float* part_o,
-                                                                    float* part_ml) {
+// CG column groups times KG key groups of wavefronts, eight: KG = 2 shares a tile's keys out where there are too few columns for eight.
+// The matrix units and the vector units of a SIMD work at the same time only if its two wavefronts (w and w + 4) are in different phases,
+// and wavefronts that meet at a barrier every tile are not.  So a tile has two phases, M (values of the tile before, scores of this
+// one) and V (softmax, loads and stores), with a barrier behind each, and the second four wavefronts are one phase behind the first.
+// In phases: K of tile t is read in 2t and 2t + 1, V of tile t in 2t + 2 and 2t + 3, so of two stages each, K of tile t + 1 and V of
+// tile t may be stored in 2t and 2t + 1: the first four store them in their V of tile t, the others in theirs of tile t - 1.
+template <int HD, int CG, int KG>
+__global__ __launch_bounds__(512, 2) void paged_attn_wide_kernel(PagedRows b, AttnRows a, int split_len, int col_tiles, float* part_o,
+                                                                float* part_ml) {
   using Cols = WideColumns<HD>;
-  constexpr int EB = Cols::EB, TILE = 64 * HD * 2;
-  extern __shared__ __attribute__((aligned(1024))) unsigned char lds[];     // two stages of (K tile, V tile)
+  using Loader = TileLoader<HD, 8, true>;
+  static_assert(CG * KG == 8, "eight wavefronts");
+  constexpr int EB = Cols::EB, TILE = 64 * HD * 2, NB = 2 / KG;
+  extern __shared__ __attribute__((aligned(1024))) unsigned char lds[];     // K, K, V, V
   const int seq = blockIdx.z, hk = blockIdx.x, group = a.Hq / b.Hkv, split = blockIdx.y / col_tiles;
-  const int wg_col0 = (blockIdx.y % col_tiles) * (NW * 32);
+  const int wg_col0 = (blockIdx.y % col_tiles) * (CG * 32);
   const SeqSpan sp = seq_span(b, seq);
   const Slice sl = slice_of(sp, split, split_len);
   if (wg_col0 >= sp.count * group || sl.key0 >= sl.key1) return;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, half = lane >> 5;
-  const bool works = wg_col0 + wave * 32 < sp.count * group;                // the others only bring tiles
+  const int cg = wave % CG, kg = wave / CG, late = wave >> 2;
+  const bool works = wg_col0 + cg * 32 < sp.count * group;                  // the others only bring tiles
+  const Loader in(b, a, sp, seq, hk, wave, lane);
+  const int tiles = (sl.key1 - sl.key0 + 63) / 64;
+
+  // pages of tiles s .. s + 2 (s: the tile whose values are asked for next)
+  int id[3][Loader::LOADS];
+  auto pages = [&](int (&x)[Loader::LOADS], int tile) __attribute__((always_inline)) {
+#pragma unroll
+    for (int i = 0; i < Loader::LOADS; ++i) x[i] = in.page_at(sl.key0 + 64 * tile + i * Loader::PASS + wave * Loader::ROWS);
+  };
+#pragma unroll
+  for (int d = 0; d < 3; ++d) pages(id[d], d);
+  typename Loader::Part k0, v0, k1, v1;
+  in.load(k0, in.kp, sl.key0, id[0]);
   Cols cols;
-  cols.start(a, sp, hk, group, wg_col0 + wave * 32 + (lane & 31), half);
-  TileLoader<HD, NW, true> in(b, a, sp, seq, hk, wave, lane);
-  in.run(lds, sl.key0, sl.key1, sp.n, [&](auto masked, int j0, uint64_t there, const unsigned char* base) __attribute__((always_inline)) {
+  cols.start(a, sp, hk, group, wg_col0 + cg * 32 + (lane & 31), half);
+  // tiles in front that every column sees whole
+  int whole = (sp.n - sl.key0) / 64;
+  whole = whole < 0 ? 0 : whole > tiles ? tiles : whole;
+  for (int i = 0; i < whole; i += 64) {                    // a lane a tile
+    bool bad = false;
+    if (i + lane < whole)
+      for (int r = 0; r < 64; r += 1 << (in.shift < 6 ? in.shift : 6))
+        bad |= (unsigned)in.table[(sl.key0 + 64 * (i + lane) + r) >> in.shift] >= (unsigned)in.n_pages;
+    const uint64_t any = __ballot(bad);
+    if (any) whole = i + __builtin_ctzll(any);
+  }
+  int next = 0;                                            // s
+  auto ask = [&](typename Loader::Part& k, typename Loader::Part& v) __attribute__((always_inline)) {
+    if (next < tiles) in.load(v, in.vp, sl.key0 + 64 * next, id[0]);
+    if (next + 1 < tiles) in.load(k, in.kp, sl.key0 + 64 * (next + 1), id[1]);
+#pragma unroll
+    for (int i = 0; i < Loader::LOADS; ++i) id[0][i] = id[1][i], id[1][i] = id[2][i];
+    pages(id[2], next + 3);
+    ++next;
+  };
+  auto store = [&](typename Loader::Part& k, typename Loader::Part& v, int s) __attribute__((always_inline)) {
+    if (s >= whole && s < tiles) in.clear(v, in.there_of(sl.key0 + 64 * s, in.pages(sl.key0 + 64 * s)));
+    if (s + 1 < tiles) in.store_k(k, lds + ((s + 1) & 1) * TILE);
+    if (s < tiles) in.store_v(v, lds + 2 * TILE + (s & 1) * TILE);
+  };
+  in.store_k(k0, lds);
+  if (late) {
+    ask(k1, v1);
+    ask(k0, v0);
+  } else {
+    ask(k0, v0);
+    ask(k1, v1);
+  }
+  __syncthreads();
+  if (late) {
+    store(k1, v1, 0);
+    ask(k1, v1);
+    __syncthreads();
+  }
+  float p[NB][16];
+  Frag pf[2 * NB];
+  const int first = NB == 1 ? kg * 32 * HD * 2 : 0;
+  if (works) cols.template scores<NB>(lds + first, p, lane);
+  __syncthreads();
+  auto step = [&](auto masked, int t, typename Loader::Part& k, typename Loader::Part& v) __attribute__((always_inline)) {
     constexpr bool MASKED = decltype(masked)::value;
-    if (!works) return;
-    const uint64_t vis = MASKED ? seen_bits(a, sp, cols.row, j0, there) : 0ull;
-    cols.template multiply<MASKED>(base, base + TILE, vis, a.scale_log2, lane);
-  });
-  if (!works) return;
+    if (works) {
+      uint64_t vis = 0;
+      if (MASKED) {
+        const int j0 = sl.key0 + 64 * t;
+        vis = seen_bits(a, sp, cols.row, j0, in.there_of(j0, in.pages(j0))) >> (NB == 1 ? 32 * kg : 0);
+      }
+      cols.template soften<MASKED, NB>(p, pf, vis, a.scale_log2, lane);
+    }
+    store(k, v, t + late);
+    ask(k, v);
+    __syncthreads();
+    if (works && !MASKED) {                                // (scores of a tile past the slice's last are nobody's)
+      cols.template advance<NB>(lds + 2 * TILE + (t & 1) * TILE + first, lds + ((t + 1) & 1) * TILE + first, pf, p, lane);
+    } else if (works) {
+      cols.template values<MASKED, NB>(lds + 2 * TILE + (t & 1) * TILE + first, pf, lane);
+      if (t + 1 < tiles) cols.template scores<NB>(lds + ((t + 1) & 1) * TILE + first, p, lane);
+    }
+    __syncthreads();
+  };
+  int t = 0;
+  for (; t + 2 <= whole; t += 2) {
+    step(std::false_type{}, t, k0, v0);
+    step(std::false_type{}, t + 1, k1, v1);
+  }
+  for (; t < tiles; ++t) {                                 // (t is even at first: the sets change places from step to step)
+    step(std::true_type{}, t, k0, v0);
+#pragma unroll
+    for (int i = 0; i < Loader::LOADS; ++i) {
+      const u32x4_t x = k0[i], y = v0[i];
+      k0[i] = k1[i], v0[i] = v1[i], k1[i] = x, v1[i] = y;
+    }
+  }
+  if (!late) __syncthreads();
   auto sw = __builtin_amdgcn_permlane32_swap(__float_as_uint(cols.l), __float_as_uint(cols.l), false, false);
-  const float sum = __uint_as_float(sw[0]) + __uint_as_float(sw[1]);
-  if (cols.row >= sp.count) return;
+  float sum = __uint_as_float(sw[0]) + __uint_as_float(sw[1]);
+  if constexpr (KG == 2) {                                 // (behind the last tile's barrier: its LDS is free)
+    float2* lds_ml = (float2*)lds;
+    lds_ml[(kg * CG + cg) * 64 + lane] = make_float2(cols.m, sum);
+    __syncthreads();
+    const float2 ml = lds_ml[((1 - kg) * CG + cg) * 64 + lane];
+    __syncthreads();
+    const float all = fmaxf(cols.m, ml.x), ref = all == -INFINITY ? 0.f : all;
+    const float mine = __builtin_amdgcn_exp2f(cols.m - ref);
+    sum = sum * mine + ml.y * __builtin_amdgcn_exp2f(ml.x - ref);
+    cols.m = all;
+#pragma unroll
+    for (int eb = 0; eb < EB; ++eb) cols.o[eb] *= mine;
+    floatx4_t* lds_o = (floatx4_t*)lds + cg * 64 * EB * 4;
+    if (works && kg) {
+#pragma unroll
+      for (int x = 0; x < EB * 4; ++x)
+        lds_o[x * 64 + lane] = floatx4_t{cols.o[x >> 2][(x & 3) * 4], cols.o[x >> 2][(x & 3) * 4 + 1], cols.o[x >> 2][(x & 3) * 4 + 2], cols.o[x >> 2][(x & 3) * 4 + 3]};
+    }
+    __syncthreads();
+    if (kg || !works) return;
+#pragma unroll
+    for (int x = 0; x < EB * 4; ++x) {
+      const floatx4_t y = lds_o[x * 64 + lane];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) cols.o[x >> 2][(x & 3) * 4 + i] += y[i];
+    }
+  }
+  if (!works || cols.row >= sp.count) return;
   const int64_t at = sp.row0 + cols.row;
   if (sl.count > 1) {
     const size_t rows = (size_t)b.rows * a.Hq;
@@ -824,7 +1033,7 @@ namespace {
 struct AttnPlan {
   int blocks;                    // column blocks of 16 a wavefront owns
   bool few, simple;
-  int col_tiles, split_len, splits;
+  int tile_cols, col_tiles, split_len, splits;
 };
 AttnPlan attn_plan(int dtype, const PagedRows& b, int Hq) {
   AttnPlan p{};
@@ -834,7 +1043,8 @@ AttnPlan attn_plan(int dtype, const PagedRows& b, int Hq) {
   if (p.simple) return p;
   p.few = cols <= 32;
   p.blocks = p.few ? (cols <= 16 ? 1 : 2) : cols <= 64 ? 1 : 2;
-  p.col_tiles = p.few ? 1 : (cols + 64 * p.blocks - 1) / (64 * p.blocks);
+  p.tile_cols = p.few ? 32 : cols <= 64 ? 64 : cols <= 128 ? 128 : 256;
+  p.col_tiles = (cols + p.tile_cols - 1) / p.tile_cols;
   const int64_t groups = (int64_t)b.seqs * b.Hkv * p.col_tiles, want = p.few ? 1024 : 512;
   const int least = p.few ? 256 : 512;
   int64_t splits = (want + groups - 1) / groups;
@@ -850,8 +1060,9 @@ template <int HD> hipError_t launch_attn_hd(const AttnPlan& p, const PagedRows& 
     auto f = p.blocks == 1 ? paged_attn_few_kernel<HD, 1> : paged_attn_few_kernel<HD, 2>;
     hipLaunchKernelGGL(f, grid, dim3(256), 0, s, b, a, p.split_len, part_o, part_ml);
   } else {
-    auto f = p.blocks == 1 ? paged_attn_tile_kernel<HD, 1, 4> : paged_attn_wide_kernel<HD, 4>;
-    hipLaunchKernelGGL(f, grid, dim3(256), 4 * 64 * HD * 2, s, b, a, p.split_len, p.col_tiles, part_o, part_ml);
+    auto f = p.tile_cols == 64 ? paged_attn_tile_kernel<HD, 1, 4> : p.tile_cols == 128 ? paged_attn_wide_kernel<HD, 4, 2> : paged_attn_wide_kernel<HD, 8, 1>;
+    hipLaunchKernelGGL(f, grid, dim3(p.tile_cols == 64 ? 256 : 512), 4 * 64 * HD * 2, s, b, a, p.split_len,
+                       p.col_tiles, part_o, part_ml);
   }
   if (p.splits > 1) {
     const dim3 rows(a.Hq, b.max_rows, b.seqs);
