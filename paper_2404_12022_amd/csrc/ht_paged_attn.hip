@@ -429,6 +429,113 @@ __device__ __forceinline__ Slice slice_of(const SeqSpan& sp, int split, int spli
   return Slice{k0, k0 + split_len < S ? k0 + split_len : S, count};
 }
 
+// Shared-out work of the kernels for many columns.  The tiles of all (head, sequence, column tile) items stand in one row, heads outermost
+// and the tiles of an item innermost, and every workgroup takes the next `quota` of them: lengths may be as ragged as they like.  An
+// item that several workgroups share leaves partial results, two places to a workgroup (an item is a workgroup's first, and keeps its place
+// 0, or its last, place 1; those between are whole).  Workgroups of one XCD (numbers that are equal modulo 8) stand next to each other:
+// column tiles of the same keys meet in one L2.
+constexpr int kShareSeqs = 256;              // sequences whose tiles a workgroup can add up (a thread each)
+struct Share {
+  int64_t before[kShareSeqs + 1];            // tiles of a head in front of sequence i
+  int64_t part[8];
+};
+__device__ __forceinline__ int64_t tiles_of(const SeqSpan& sp, int group, int cols) {
+  return sp.count ? (int64_t)((sp.n + sp.count + 63) / 64) * ((sp.count * group + cols - 1) / cols) : 0;
+}
+// Fills `sh`; the tiles of a head.  All threads of the workgroup, 256 or more.
+__device__ __forceinline__ int64_t share_out(Share& sh, const PagedRows& b, int group, int cols) {
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const int64_t mine = tid < b.seqs && tid < kShareSeqs ? tiles_of(seq_span(b, tid), group, cols) : 0;
+  int64_t run = mine;
+#pragma unroll
+  for (int o = 1; o < 64; o <<= 1) {
+    const int64_t other = __shfl_up((long long)run, o, 64);
+    if (lane >= o) run += other;
+  }
+  if (lane == 63) sh.part[wave] = run;
+  __syncthreads();
+  int64_t front = 0;
+  for (int w = 0; w < wave; ++w) front += sh.part[w];
+  if (tid < kShareSeqs) sh.before[tid + 1] = front + run;
+  if (tid == 0) sh.before[0] = 0;
+  __syncthreads();
+  return sh.before[b.seqs];
+}
+__device__ __forceinline__ int64_t quota_of(int64_t head_tiles, int Hkv, int workgroups, int least) {
+  const int64_t q = (head_tiles * Hkv + workgroups - 1) / workgroups;
+  return q > least ? q : least;
+}
+// The last sequence that starts at or before tile `at` and has tiles; every lane
+__device__ __forceinline__ int sequence_at(const Share& sh, int seqs, int64_t at, int lane) {
+  int seq = 0;
+  for (int i = 0; i < seqs; i += 64) seq += __popcll(__ballot(i + lane < seqs && sh.before[i + lane + 1] <= at));
+  return seq;
+}
+__device__ __forceinline__ int64_t uniform(int64_t v) {
+  return (int64_t)((uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((int)(v >> 32)) << 32 | (uint32_t)__builtin_amdgcn_readfirstlane((int)v));
+}
+// One item's part in a workgroup's row of tiles
+struct Segment {
+  int seq, hk, col_tile, key0, key1;
+  bool whole;
+  int place;                                 // of the partial result, if not whole
+};
+__device__ __forceinline__ Segment segment_at(const Share& sh, const PagedRows& b, int64_t head_tiles, int64_t u, int64_t end, int64_t begin,
+                                              int workgroup, int lane) {
+  Segment s;
+  s.hk = (int)(u / head_tiles);
+  const int64_t at = u - s.hk * head_tiles;
+  s.seq = __builtin_amdgcn_readfirstlane(sequence_at(sh, b.seqs, at, lane));
+  const SeqSpan sp = seq_span(b, s.seq);
+  const int tiles = (sp.n + sp.count + 63) / 64;
+  const int64_t in = at - uniform(sh.before[s.seq]);
+  s.col_tile = (int)(in / tiles);
+  const int first = (int)(in - (int64_t)s.col_tile * tiles);
+  const int64_t left = end - u;
+  const int count = left < tiles - first ? (int)left : tiles - first;
+  s.key0 = first * 64;
+  s.key1 = (first + count) * 64 < sp.n + sp.count ? (first + count) * 64 : sp.n + sp.count;
+  s.whole = count == tiles;
+  s.place = workgroup * 2 + (u == begin ? 0 : 1);
+  return s;
+}
+__device__ __forceinline__ int shared_workgroup() {         // the number of this workgroup in the row
+  const int w = blockIdx.x, per = gridDim.x / 8;
+  return gridDim.x % 8 ? w : w % 8 * per + w / 8;
+}
+
+// The segments of this workgroup, one after the other
+template <int COLS, typename F>
+__device__ __forceinline__ void shared_items(Share& sh, const PagedRows& b, const AttnRows& a, int least, F&& item) {
+  const int group = a.Hq / b.Hkv;
+  const bool alone = b.seqs > kShareSeqs;                  // an item to a workgroup
+  int64_t head_tiles = 1, begin = 0, end = 1;
+  const int w = shared_workgroup();
+  if (!alone) {
+    head_tiles = uniform(share_out(sh, b, group, COLS));
+    if (!head_tiles) return;
+    const int64_t quota = quota_of(head_tiles, b.Hkv, gridDim.x, least), all = head_tiles * b.Hkv;
+    begin = w * quota;
+    end = begin + quota < all ? begin + quota : all;
+  }
+  for (int64_t u = begin; u < end;) {
+    Segment s;
+    if (alone) {
+      const SeqSpan sp = seq_span(b, blockIdx.z);
+      if ((int)blockIdx.y * COLS >= sp.count * group) return;
+      s = Segment{(int)blockIdx.z, (int)blockIdx.x, (int)blockIdx.y, 0, sp.n + sp.count, true, 0};
+    } else {
+      s = segment_at(sh, b, head_tiles, u, end, begin, w, threadIdx.x & 63);
+    }
+    int lane = threadIdx.x & 63;
+    asm volatile("" : "+v"(lane));                         // what an item works out from it is not kept from item to item
+    item(s, lane);
+    u += (s.key1 - s.key0 + 63) / 64;
+    if (alone) return;
+    __syncthreads();                                       // (the next one's tiles go where the last one's are read)
+  }
+}
+
 }  // namespace
 
 // Up to 32 columns: the four wavefronts of a workgroup take blocks of 32 keys in turn, each for itself (no barrier until the end),
@@ -568,51 +675,53 @@ __global__ __launch_bounds__(256, 2) void paged_attn_few_kernel(PagedRows b, Att
 
 // More columns: every wavefront owns QB blocks of 16, tiles of 64 keys of K and V go through LDS for all of them.
 template <int HD, int QB, int NW>
-__global__ __launch_bounds__(64 * NW, 2) void paged_attn_tile_kernel(PagedRows b, AttnRows a, int split_len, int col_tiles, float* part_o,
-                                                                    float* part_ml) {
+__global__ __launch_bounds__(64 * NW, 2) void paged_attn_tile_kernel(PagedRows b, AttnRows a, int least, float* part_o, float* part_ml) {
   using Cols = Columns<HD, QB>;
-  constexpr int EB = Cols::EB, TILE = 64 * HD * 2;
-  extern __shared__ __attribute__((aligned(1024))) unsigned char lds[];     // two stages of (K tile, V tile)
-  const int seq = blockIdx.z, hk = blockIdx.x, group = a.Hq / b.Hkv, split = blockIdx.y / col_tiles;
-  const int wg_col0 = (blockIdx.y % col_tiles) * (NW * QB * 16);
-  const SeqSpan sp = seq_span(b, seq);
-  const Slice sl = slice_of(sp, split, split_len);
-  if (wg_col0 >= sp.count * group || sl.key0 >= sl.key1) return;
-  const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, r16 = lane & 15, g = lane >> 4;
-  const bool works = wg_col0 + wave * QB * 16 < sp.count * group;          // the others only bring tiles
-
-  Cols cols;
-  cols.start(a, sp, hk, group, wg_col0 + wave * QB * 16, r16, g);
-  const TileLoader<HD, NW, false> in(b, a, sp, seq, hk, wave, lane);
-  in.run(lds, sl.key0, sl.key1, sp.n, [&](auto masked, int j0, uint64_t there, const unsigned char* base) __attribute__((always_inline)) {
-    constexpr bool MASKED = decltype(masked)::value;
+  constexpr int EB = Cols::EB, TILE = 64 * HD * 2, COLS = NW * QB * 16;
+  __shared__ __attribute__((aligned(1024))) unsigned char lds[4 * TILE];   // two stages of (K tile, V tile)
+  __shared__ Share sh;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), group = a.Hq / b.Hkv;
+  auto item = [&](const Segment& s, int lane) __attribute__((always_inline)) {
+    const int r16 = lane & 15, g = lane >> 4;
+    const SeqSpan sp = seq_span(b, s.seq);
+    const int col0 = s.col_tile * COLS + wave * QB * 16;
+    const bool works = col0 < sp.count * group;            // the others only bring tiles
+    Cols cols;
+    cols.start(a, sp, s.hk, group, col0, r16, g);
+    const TileLoader<HD, NW, false> in(b, a, sp, s.seq, s.hk, wave, lane);
+    in.run(lds, s.key0, s.key1, sp.n, [&](auto masked, int j0, uint64_t there, const unsigned char* base) __attribute__((always_inline)) {
+      constexpr bool MASKED = decltype(masked)::value;
+      if (!works) return;
+      const int krow = 8 * (r16 >> 2) + (r16 & 3);
+      auto k_of = [&](int sub, int bl, int es) __attribute__((always_inline)) {
+        const int row = sub * 32 + 4 * bl + krow;
+        Frag f;
+        f.nat = *(const u32x4_t*)(base + row * (HD * 2) + k_place<HD>(row, es * 4 + g));
+        return f;
+      };
+      uint64_t vis[QB] = {};
+      if (MASKED) {
+#pragma unroll
+        for (int qb = 0; qb < QB; ++qb) vis[qb] = seen_bits(a, sp, cols.row[qb], j0, there);
+      }
+      cols.template multiply<2, MASKED>(k_of, base + TILE, vis, a.scale_log2, r16, g);
+    });
     if (!works) return;
-    const int krow = 8 * (r16 >> 2) + (r16 & 3);
-    auto k_of = [&](int sub, int bl, int es) __attribute__((always_inline)) {
-      const int row = sub * 32 + 4 * bl + krow;
-      Frag f;
-      f.nat = *(const u32x4_t*)(base + row * (HD * 2) + k_place<HD>(row, es * 4 + g));
-      return f;
-    };
-    uint64_t vis[QB] = {};
-    if (MASKED) {
 #pragma unroll
-      for (int qb = 0; qb < QB; ++qb) vis[qb] = seen_bits(a, sp, cols.row[qb], j0, there);
+    for (int qb = 0; qb < QB; ++qb) {
+      const float sum = sum_over_groups(cols.l[qb]);
+      if (s.whole) {
+#pragma unroll
+        for (int eb = 0; eb < EB; ++eb) cols.finish(a, sp, qb, cols.o[qb][eb], eb, sum, g, nullptr);
+      } else {
+        const size_t at = (size_t)s.place * COLS + (wave * QB + qb) * 16 + r16;
+#pragma unroll
+        for (int eb = 0; eb < EB; ++eb) *(floatx4_t*)(part_o + at * HD + eb * 16 + g * 4) = cols.o[qb][eb];
+        if (g == 0) *(float2*)(part_ml + at * 2) = make_float2(cols.m[qb], sum);
+      }
     }
-    cols.template multiply<2, MASKED>(k_of, base + TILE, vis, a.scale_log2, r16, g);
-  });
-
-  if (!works) return;
-  const bool split_out = sl.count > 1;
-  float* po = split_out ? part_o + (size_t)split * b.rows * a.Hq * HD : nullptr;
-  float* pml = split_out ? part_ml + (size_t)split * b.rows * a.Hq * 2 : nullptr;
-#pragma unroll
-  for (int qb = 0; qb < QB; ++qb) {
-    const float sum = sum_over_groups(cols.l[qb]);
-#pragma unroll
-    for (int eb = 0; eb < EB; ++eb) cols.finish(a, sp, qb, cols.o[qb][eb], eb, sum, g, po);
-    if (split_out && g == 0) cols.finish_sum(a, sp, qb, cols.m[qb], sum, pml);
-  }
+  };
+  shared_items<COLS>(sh, b, a, least, item);
 }
 
 // Many columns: 32 to a wavefront, on the 32 x 32 x 16 instructions (half as many to issue, and a column lies in two lanes instead of
@@ -806,20 +915,19 @@ template <int HD> struct WideColumns {
 // In phases: K of tile t is read in 2t and 2t + 1, V of tile t in 2t + 2 and 2t + 3, so of two stages each, K of tile t + 1 and V of
 // tile t may be stored in 2t and 2t + 1: the first four store them in their V of tile t, the others in theirs of tile t - 1.
 template <int HD, int CG, int KG>
-__global__ __launch_bounds__(512, 2) void paged_attn_wide_kernel(PagedRows b, AttnRows a, int split_len, int col_tiles, float* part_o,
-                                                                float* part_ml) {
+__global__ __launch_bounds__(512, 2) void paged_attn_wide_kernel(PagedRows b, AttnRows a, int least, float* part_o, float* part_ml) {
   using Cols = WideColumns<HD>;
   using Loader = TileLoader<HD, 8, true>;
   static_assert(CG * KG == 8, "eight wavefronts");
-  constexpr int EB = Cols::EB, TILE = 64 * HD * 2, NB = 2 / KG;
-  extern __shared__ __attribute__((aligned(1024))) unsigned char lds[];     // K, K, V, V
-  const int seq = blockIdx.z, hk = blockIdx.x, group = a.Hq / b.Hkv, split = blockIdx.y / col_tiles;
-  const int wg_col0 = (blockIdx.y % col_tiles) * (CG * 32);
-  const SeqSpan sp = seq_span(b, seq);
-  const Slice sl = slice_of(sp, split, split_len);
-  if (wg_col0 >= sp.count * group || sl.key0 >= sl.key1) return;
-  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, half = lane >> 5;
-  const int cg = wave % CG, kg = wave / CG, late = wave >> 2;
+  constexpr int EB = Cols::EB, TILE = 64 * HD * 2, NB = 2 / KG, COLS = CG * 32;
+  __shared__ __attribute__((aligned(1024))) unsigned char lds[4 * TILE];   // K, K, V, V
+  __shared__ Share sh;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int cg = wave % CG, kg = wave / CG, late = wave >> 2, group = a.Hq / b.Hkv;
+  auto item = [&](const Segment& sl, int lane) __attribute__((always_inline)) {
+  const int half = lane >> 5;
+  const SeqSpan sp = seq_span(b, sl.seq);
+  const int seq = sl.seq, hk = sl.hk, wg_col0 = sl.col_tile * COLS;
   const bool works = wg_col0 + cg * 32 < sp.count * group;                  // the others only bring tiles
   const Loader in(b, a, sp, seq, hk, wave, lane);
   const int tiles = (sl.key1 - sl.key0 + 63) / 64;
@@ -936,7 +1044,7 @@ __global__ __launch_bounds__(512, 2) void paged_attn_wide_kernel(PagedRows b, At
         lds_o[x * 64 + lane] = floatx4_t{cols.o[x >> 2][(x & 3) * 4], cols.o[x >> 2][(x & 3) * 4 + 1], cols.o[x >> 2][(x & 3) * 4 + 2], cols.o[x >> 2][(x & 3) * 4 + 3]};
     }
     __syncthreads();
-    if (kg || !works) return;
+    if (kg) return;
 #pragma unroll
     for (int x = 0; x < EB * 4; ++x) {
       const floatx4_t y = lds_o[x * 64 + lane];
@@ -944,20 +1052,19 @@ __global__ __launch_bounds__(512, 2) void paged_attn_wide_kernel(PagedRows b, At
       for (int i = 0; i < 4; ++i) cols.o[x >> 2][(x & 3) * 4 + i] += y[i];
     }
   }
-  if (!works || cols.row >= sp.count) return;
-  const int64_t at = sp.row0 + cols.row;
-  if (sl.count > 1) {
-    const size_t rows = (size_t)b.rows * a.Hq;
-    float* po = part_o + (split * rows + at * a.Hq + cols.head) * HD + half * 4;
+  if (!works) return;
+  if (!sl.whole) {
+    const size_t at = (size_t)sl.place * COLS + cg * 32 + (lane & 31);
+    float* po = part_o + at * HD + half * 4;
 #pragma unroll
     for (int eb = 0; eb < EB; ++eb)
 #pragma unroll
       for (int a4 = 0; a4 < 4; ++a4)
         *(float4*)(po + eb * 32 + a4 * 8) = make_float4(cols.o[eb][a4 * 4], cols.o[eb][a4 * 4 + 1], cols.o[eb][a4 * 4 + 2], cols.o[eb][a4 * 4 + 3]);
-    if (half == 0) *(float2*)(part_ml + (split * rows + at * a.Hq + cols.head) * 2) = make_float2(cols.m, sum);
-  } else {
+    if (half == 0) *(float2*)(part_ml + at * 2) = make_float2(cols.m, sum);
+  } else if (cols.row < sp.count) {
     const float inv = sum == 0.f ? 0.f : 1.0f / sum;
-    bf16_t* out = (bf16_t*)a.out + at * a.out_stride + (int64_t)cols.head * HD + half * 4;
+    bf16_t* out = (bf16_t*)a.out + (int64_t)(sp.row0 + cols.row) * a.out_stride + (int64_t)cols.head * HD + half * 4;
 #pragma unroll
     for (int eb = 0; eb < EB; ++eb)
 #pragma unroll
@@ -965,6 +1072,8 @@ __global__ __launch_bounds__(512, 2) void paged_attn_wide_kernel(PagedRows b, At
         ((Loose8*)(out + eb * 32 + a4 * 8))->v = sum == 0.f ? make_uint2(0, 0) :
             pack4_bf16(cols.o[eb][a4 * 4] * inv, cols.o[eb][a4 * 4 + 1] * inv, cols.o[eb][a4 * 4 + 2] * inv, cols.o[eb][a4 * 4 + 3] * inv);
   }
+  };
+  shared_items<COLS>(sh, b, a, least, item);
 }
 
 // out = sum_s 2^(m_s - m) O_s / sum_s 2^(m_s - m) l_s over the slices of a sequence, in a fixed order.  A workgroup per (row, head) and
@@ -1028,12 +1137,59 @@ __global__ __launch_bounds__(PARTS * (HD / 4)) void paged_attn_join_kernel(Paged
       sum == 0.f ? make_uint2(0, 0) : pack4_bf16(acc[0] * inv, acc[1] * inv, acc[2] * inv, acc[3] * inv);
 }
 
+// The same for shared-out work: the partial results of an item, workgroup after workgroup.  A workgroup of 256 threads per row and 256 /
+// (HD / 4) query heads.
+template <int HD, int COLS>
+__global__ __launch_bounds__(256) void paged_attn_share_join_kernel(PagedRows b, AttnRows a, int workgroups, int least, const float* part_o,
+                                                                   const float* part_ml) {
+  __shared__ Share sh;
+  constexpr int T = HD / 4;
+  const int seq = blockIdx.z, row = blockIdx.y, head = blockIdx.x * (256 / T) + threadIdx.x / T, e = threadIdx.x % T * 4;
+  const SeqSpan sp = seq_span(b, seq);
+  if (row >= sp.count) return;
+  const int group = a.Hq / b.Hkv;
+  const int64_t head_tiles = share_out(sh, b, group, COLS);
+  if (head >= a.Hq) return;
+  const int64_t quota = quota_of(head_tiles, b.Hkv, workgroups, least);
+  const int tiles = (sp.n + sp.count + 63) / 64, hk = head / group, col = row * group + head % group;
+  const int64_t u0 = hk * head_tiles + sh.before[seq] + (int64_t)(col / COLS) * tiles, w0 = u0 / quota, w1 = (u0 + tiles - 1) / quota;
+  if (w0 == w1) return;                                    // one workgroup had it whole
+  auto place = [&](int64_t w) { return (size_t)(w * 2 + (w * quota >= u0 ? 0 : 1)) * COLS + col % COLS; };
+  float top = -INFINITY, sum = 0.f;
+  floatx4_t acc = floatx4_t{0.f, 0.f, 0.f, 0.f};
+  constexpr int NS = 4;                                    // requested at a time
+  for (int64_t w = w0; w <= w1; w += NS) {
+    float2 ml[NS];
+    floatx4_t x[NS];
+#pragma unroll
+    for (int i = 0; i < NS; ++i) {
+      const size_t at = place(w + i <= w1 ? w + i : w);
+      ml[i] = *(const float2*)(part_ml + at * 2);
+      x[i] = *(const floatx4_t*)(part_o + at * HD + e);
+    }
+#pragma unroll
+    for (int i = 0; i < NS; ++i) {
+      if (w + i > w1) break;
+      const float now = fmaxf(top, ml[i].x), ref = now == -INFINITY ? 0.f : now;
+      const float old = __builtin_amdgcn_exp2f(top - ref), f = __builtin_amdgcn_exp2f(ml[i].x - ref);
+      sum = fmaf(f, ml[i].y, sum * old);
+#pragma unroll
+      for (int c = 0; c < 4; ++c) acc[c] = fmaf(f, x[i][c], acc[c] * old);
+      top = now;
+    }
+  }
+  const float inv = sum == 0.f ? 0.f : 1.0f / sum;
+  ((Loose8*)((bf16_t*)a.out + (int64_t)(sp.row0 + row) * a.out_stride + (int64_t)head * HD + e))->v =
+      sum == 0.f ? make_uint2(0, 0) : pack4_bf16(acc[0] * inv, acc[1] * inv, acc[2] * inv, acc[3] * inv);
+}
+
 namespace {
 // How a call runs: from its bounds alone, so that a captured call fits whatever its tables say later
 struct AttnPlan {
-  int blocks;                    // column blocks of 16 a wavefront owns
-  bool few, simple;
-  int tile_cols, col_tiles, split_len, splits;
+  bool simple, few;
+  int blocks;                    // few: column blocks of 16
+  int split_len, splits;         // few
+  int cols, workgroups, least;   // shared-out work: columns of an item, workgroups (0: one to an item), tiles that are worth one
 };
 AttnPlan attn_plan(int dtype, const PagedRows& b, int Hq) {
   AttnPlan p{};
@@ -1042,40 +1198,55 @@ AttnPlan attn_plan(int dtype, const PagedRows& b, int Hq) {
   p.split_len = S, p.splits = 1;
   if (p.simple) return p;
   p.few = cols <= 32;
-  p.blocks = p.few ? (cols <= 16 ? 1 : 2) : cols <= 64 ? 1 : 2;
-  p.tile_cols = p.few ? 32 : cols <= 64 ? 64 : cols <= 128 ? 128 : 256;
-  p.col_tiles = (cols + p.tile_cols - 1) / p.tile_cols;
-  const int64_t groups = (int64_t)b.seqs * b.Hkv * p.col_tiles, want = p.few ? 1024 : 512;
-  const int least = p.few ? 256 : 512;
-  int64_t splits = (want + groups - 1) / groups;
-  if (splits > S / least) splits = S / least;
-  if (splits < 1) splits = 1;
-  p.split_len = (int)(((S + splits - 1) / splits + 63) / 64 * 64);
-  p.splits = (S + p.split_len - 1) / p.split_len;
+  if (p.few) {
+    p.blocks = cols <= 16 ? 1 : 2;
+    const int64_t groups = (int64_t)b.seqs * b.Hkv, want = 1024;
+    const int least = 256;
+    int64_t splits = (want + groups - 1) / groups;
+    if (splits > S / least) splits = S / least;
+    if (splits < 1) splits = 1;
+    p.split_len = (int)(((S + splits - 1) / splits + 63) / 64 * 64);
+    p.splits = (S + p.split_len - 1) / p.split_len;
+    return p;
+  }
+  p.cols = cols <= 64 ? 64 : cols <= 128 ? 128 : 256;
+  p.least = 4;
+  const int64_t most = (int64_t)b.seqs * b.Hkv * ((cols + p.cols - 1) / p.cols) * ((S + 63) / 64);        // tiles
+  p.workgroups = b.seqs > kShareSeqs ? 0 : p.cols == 64 ? 512 : 256;
+  if (p.workgroups > (most + p.least - 1) / p.least) p.workgroups = (int)((most + p.least - 1) / p.least);
   return p;
 }
+size_t part_columns(const AttnPlan& p, const PagedRows& b, int Hq) {        // columns of partial results
+  if (p.simple) return 0;
+  if (p.few) return p.splits > 1 ? (size_t)p.splits * b.rows * Hq : 0;
+  return (size_t)p.workgroups * 2 * p.cols;
+}
 template <int HD> hipError_t launch_attn_hd(const AttnPlan& p, const PagedRows& b, const AttnRows& a, float* part_o, float* part_ml, hipStream_t s) {
-  const dim3 grid(b.Hkv, p.splits * p.col_tiles, b.seqs);
   if (p.few) {
     auto f = p.blocks == 1 ? paged_attn_few_kernel<HD, 1> : paged_attn_few_kernel<HD, 2>;
-    hipLaunchKernelGGL(f, grid, dim3(256), 0, s, b, a, p.split_len, part_o, part_ml);
-  } else {
-    auto f = p.tile_cols == 64 ? paged_attn_tile_kernel<HD, 1, 4> : p.tile_cols == 128 ? paged_attn_wide_kernel<HD, 4, 2> : paged_attn_wide_kernel<HD, 8, 1>;
-    hipLaunchKernelGGL(f, grid, dim3(p.tile_cols == 64 ? 256 : 512), 4 * 64 * HD * 2, s, b, a, p.split_len,
-                       p.col_tiles, part_o, part_ml);
+    hipLaunchKernelGGL(f, dim3(b.Hkv, p.splits, b.seqs), dim3(256), 0, s, b, a, p.split_len, part_o, part_ml);
+    if (p.splits > 1) {
+      const dim3 rows(a.Hq, b.max_rows, b.seqs);
+      if (p.splits > 4) hipLaunchKernelGGL((paged_attn_join_kernel<HD, 8>), rows, dim3(8 * HD / 4), 0, s, b, a, p.split_len, part_o, part_ml);
+      else hipLaunchKernelGGL((paged_attn_join_kernel<HD, 1>), rows, dim3(HD / 4), 0, s, b, a, p.split_len, part_o, part_ml);
+    }
+    return hipGetLastError();
   }
-  if (p.splits > 1) {
-    const dim3 rows(a.Hq, b.max_rows, b.seqs);
-    if (p.splits > 4) hipLaunchKernelGGL((paged_attn_join_kernel<HD, 8>), rows, dim3(8 * HD / 4), 0, s, b, a, p.split_len, part_o, part_ml);
-    else hipLaunchKernelGGL((paged_attn_join_kernel<HD, 1>), rows, dim3(HD / 4), 0, s, b, a, p.split_len, part_o, part_ml);
+  const int cols = b.max_rows * (a.Hq / b.Hkv);
+  const dim3 grid = p.workgroups ? dim3(p.workgroups) : dim3(b.Hkv, (cols + p.cols - 1) / p.cols, b.seqs);
+  auto f = p.cols == 64 ? paged_attn_tile_kernel<HD, 1, 4> : p.cols == 128 ? paged_attn_wide_kernel<HD, 4, 2> : paged_attn_wide_kernel<HD, 8, 1>;
+  hipLaunchKernelGGL(f, grid, dim3(p.cols == 64 ? 256 : 512), 0, s, b, a, p.least, part_o, part_ml);
+  if (p.workgroups > 1) {
+    auto j = p.cols == 64 ? paged_attn_share_join_kernel<HD, 64> : p.cols == 128 ? paged_attn_share_join_kernel<HD, 128> : paged_attn_share_join_kernel<HD, 256>;
+    constexpr int heads = 256 / (HD / 4);
+    hipLaunchKernelGGL(j, dim3((a.Hq + heads - 1) / heads, b.max_rows, b.seqs), dim3(256), 0, s, b, a, p.workgroups, p.least, part_o, part_ml);
   }
   return hipGetLastError();
 }
 }  // namespace
 
 size_t paged_attn_scratch_bytes(int dtype, const PagedRows& b, int Hq) {
-  const AttnPlan p = attn_plan(dtype, b, Hq);
-  return p.splits > 1 ? (size_t)p.splits * b.rows * Hq * (b.hd + 2) * sizeof(float) : 0;
+  return part_columns(attn_plan(dtype, b, Hq), b, Hq) * (b.hd + 2) * sizeof(float);
 }
 
 hipError_t launch_paged_attn(int dtype, const PagedRows& b, const AttnRows& a, void* scratch, hipStream_t s) {
@@ -1087,7 +1258,7 @@ hipError_t launch_paged_attn(int dtype, const PagedRows& b, const AttnRows& a, v
     return hipGetLastError();
   }
   float* part_o = (float*)scratch;
-  float* part_ml = part_o + (size_t)p.splits * b.rows * a.Hq * b.hd;
+  float* part_ml = part_o + part_columns(p, b, a.Hq) * b.hd;
   return b.hd == 64 ? launch_attn_hd<64>(p, b, a, part_o, part_ml, s) : launch_attn_hd<128>(p, b, a, part_o, part_ml, s);
 }
 
