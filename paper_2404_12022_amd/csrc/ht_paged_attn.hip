@@ -139,16 +139,15 @@ template <int HD> __device__ __forceinline__ Frag v_operand(const unsigned char*
   return f;
 }
 
-// Keys j0 .. j0 + 63 that row `row` of the sequence sees, as bits; `there`: those that are
-__device__ __forceinline__ uint64_t seen_bits(const AttnRows& a, const SeqSpan& sp, int row, int j0, uint64_t there) {
+// Keys j0 .. j0 + 63 that row `row` of the sequence sees, as bits; w: its mask (NULL: a chain), `there`: the keys that are
+__device__ __forceinline__ uint64_t seen_bits(const uint64_t* w, const SeqSpan& sp, int row, int j0, uint64_t there) {
   const int first = j0 - sp.n;                             // the row of the pass that key j0 is
   if (first <= -64 || row >= sp.count) return there;
   uint64_t bits;
-  if (!a.anc) {
+  if (!w) {
     const int upto = row - first;                          // rows 0 .. row
     bits = upto < 0 ? 0ull : upto >= 63 ? ~0ull : (2ull << upto) - 1;
   } else {
-    const uint64_t* w = a.anc + (size_t)(sp.row0 + row) * kMaskWords;
     if (first < 0) {
       bits = w[0] << -first | ((1ull << -first) - 1);
     } else {
@@ -159,39 +158,74 @@ __device__ __forceinline__ uint64_t seen_bits(const AttnRows& a, const SeqSpan& 
   }
   return bits & there;
 }
+__device__ __forceinline__ const uint64_t* mask_of(const AttnRows& a, const SeqSpan& sp, int row) {
+  return a.anc ? a.anc + (size_t)(sp.row0 + (row < sp.count ? row : 0)) * kMaskWords : nullptr;
+}
 // Values that are no numbers become 0 (they would reach columns that do not see them); whether there were any
-__device__ __forceinline__ bool clear_odd(Frag& f) {
+__device__ __forceinline__ bool tidy(u32x4_t& x) {
   bool odd = false;
 #pragma unroll
   for (int w = 0; w < 4; ++w) {
-    const bool lo = (f.u[w] & 0x7f80u) == 0x7f80u, hi = (f.u[w] & 0x7f800000u) == 0x7f800000u;
+    const bool lo = (x[w] & 0x7f80u) == 0x7f80u, hi = (x[w] & 0x7f800000u) == 0x7f800000u;
     odd |= lo | hi;
-    f.u[w] &= (lo ? 0u : 0xffffu) | (hi ? 0u : 0xffff0000u);
+    x[w] &= (lo ? 0u : 0xffffu) | (hi ? 0u : 0xffff0000u);
   }
   return odd;
 }
+// Four values of a key that one or more columns see, of which those that are no numbers have been left out: added (a share of one is itself)
+template <typename F> __device__ __forceinline__ void add_odd(const char* at, F&& add) {
+  const uint2 four = ((const Loose8*)at)->v;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const uint32_t v = (i < 2 ? four.x : four.y) >> (i & 1) * 16 & 0xffffu;
+    if ((v & 0x7f80u) == 0x7f80u) add(i, __uint_as_float(v << 16));
+  }
+}
+// The pages of a sequence, seen from one key/value head
+struct PageView {
+  const char *kp, *vp;
+  const int32_t* table;
+  size_t page_bytes;
+  int S, shift, n_pages;
+  __device__ __forceinline__ PageView(const PagedRows& b, const AttnRows& a, const SeqSpan& sp, int seq, int hk)
+      : table(b.table + (size_t)seq * b.table_width), S(sp.n + sp.count), shift(b.page_shift), n_pages(b.n_pages) {
+    page_bytes = (size_t)b.Hkv * b.hd * 2 << shift;
+    const size_t head = (size_t)hk * b.hd * 2 << shift;
+    kp = (const char*)a.k_pages + head;
+    vp = (const char*)a.v_pages + head;
+  }
+  // of a slot that is the same for the whole wavefront, through scalar registers
+  __device__ __forceinline__ int page_at(int slot) const {
+    const auto* in = (const __attribute__((address_space(4))) int32_t*)(uintptr_t)table;
+    return in[(slot < S ? slot : S - 1) >> shift];
+  }
+  // the keys j0 .. j0 + 63 that are there (j0 < S), as bits
+  __device__ __forceinline__ uint64_t up_to_end(int j0) const { return j0 + 64 > S ? (1ull << (S - j0)) - 1 : ~0ull; }
+  __device__ __forceinline__ uint64_t there_at(int j0) const {
+    uint64_t t = 0;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) t |= (unsigned)page_at(j0 + 8 * i) < (unsigned)n_pages ? 0xffull << 8 * i : 0ull;
+    return t & up_to_end(j0);
+  }
+  __device__ __forceinline__ const char* value_row(int slot, int hd) const {
+    return vp + page_at(slot) * page_bytes + (size_t)(slot & ((1 << shift) - 1)) * (hd * 2);
+  }
+};
+
 // The K place of the kernel with 32 columns to a wavefront, which reads 16 consecutive keys of one piece at a time
 template <int HD> __device__ __forceinline__ int wide_k_place(int row, int piece) {
   return (piece ^ (HD == 128 ? row & 15 : (row >> 1) & 7)) << 4;
 }
 
 // What a workgroup's NW wavefronts bring of a sequence's pages: tiles of 64 keys of K and V, through registers to LDS
-template <int HD, int NW, bool WIDE> struct TileLoader {
+template <int HD, int NW> struct TileLoader : PageView {
   static constexpr int PIECES = HD / 8, ROWS = 64 / PIECES, PASS = NW * ROWS, LOADS = 64 / PASS, TILE = 64 * HD * 2;
   static_assert(64 % PASS == 0, "whole passes");
   typedef u32x4_t Part[LOADS];                              // a wavefront's part of a tile
-  const char *kp, *vp;
-  const int32_t* table;
-  size_t page_bytes;
-  int S, shift, n_pages, wave, lane;
+  int wave, lane;
 
   __device__ __forceinline__ TileLoader(const PagedRows& b, const AttnRows& a, const SeqSpan& sp, int seq, int hk, int wave, int lane)
-      : table(b.table + (size_t)seq * b.table_width), S(sp.n + sp.count), shift(b.page_shift), n_pages(b.n_pages), wave(wave), lane(lane) {
-    page_bytes = (size_t)b.Hkv * HD * 2 << shift;
-    const size_t head = (size_t)hk * HD * 2 << shift;
-    kp = (const char*)a.k_pages + head;
-    vp = (const char*)a.v_pages + head;
-  }
+      : PageView(b, a, sp, seq, hk), wave(wave), lane(lane) {}
   __device__ __forceinline__ int pages(int j0) const {      // of key j0 + lane
     const int slot = j0 + lane;
     return table[(slot < S ? slot : S - 1) >> shift];
@@ -206,24 +240,11 @@ template <int HD, int NW, bool WIDE> struct TileLoader {
       x[p] = ((const Loose16*)(pool + at + (uint32_t)lane * 16u))->v;
     }
   }
-  // The same with the pages of the wavefront's rows in scalar registers
-  __device__ __forceinline__ int page_at(int slot) const {
-    const auto* in = (const __attribute__((address_space(4))) int32_t*)(uintptr_t)table;
-    return in[(slot < S ? slot : S - 1) >> shift];
-  }
-  __device__ __forceinline__ void load(Part& x, const char* pool, int j0, const int (&id)[LOADS]) const {
-#pragma unroll
-    for (int p = 0; p < LOADS; ++p) {
-      const int row0 = p * PASS + wave * ROWS, held = (unsigned)id[p] < (unsigned)n_pages ? id[p] : 0;
-      const size_t at = held * page_bytes + (size_t)((j0 + row0) & ((1 << shift) - 1)) * (HD * 2);
-      x[p] = ((const Loose16*)(pool + at + (uint32_t)lane * 16u))->v;
-    }
-  }
   __device__ __forceinline__ void store_k(const Part& x, unsigned char* base) const {
 #pragma unroll
     for (int p = 0; p < LOADS; ++p) {
       const int row = p * PASS + wave * ROWS + lane / PIECES, piece = lane % PIECES;
-      *(u32x4_t*)(base + row * (HD * 2) + (WIDE ? wide_k_place<HD>(row, piece) : k_place<HD>(row, piece))) = x[p];
+      *(u32x4_t*)(base + row * (HD * 2) + k_place<HD>(row, piece)) = x[p];
     }
   }
   __device__ __forceinline__ void store_v(const Part& x, unsigned char* base) const {
@@ -233,18 +254,25 @@ template <int HD, int NW, bool WIDE> struct TileLoader {
       *(u32x4_t*)(base + row * (HD * 2) + v_place<HD>(row, piece >> 1) + (piece & 1) * 16) = x[p];
     }
   }
-  __device__ __forceinline__ void clear(Part& x, uint64_t there) const {  // values of keys that are not there: 0 times what lies there is no 0
+  // Values for a tile that not every column sees whole: those of keys that are not there become 0 (0 times what lies there is no 0),
+  // and those that are no numbers, for add_odd; whether there were such
+  __device__ __forceinline__ bool clear(Part& x, uint64_t there, int lane) const {
+    bool odd = false;
 #pragma unroll
-    for (int p = 0; p < LOADS; ++p)
+    for (int p = 0; p < LOADS; ++p) {
       if (!(there >> (p * PASS + wave * ROWS + lane / PIECES) & 1)) x[p] = u32x4_t{0, 0, 0, 0};
+      odd |= tidy(x[p]);
+    }
+    return odd;
   }
   // Tile after tile, the next on its way while one is multiplied, two stages of (K, V), a barrier per tile; a loop for the tiles that
   // every column sees whole, and one for those behind (they hold rows of the pass; or a page is missing):
-  // f(masked, first key, keys that are there, tile)
-  template <typename F> __device__ __forceinline__ void run(unsigned char* lds, int key0, int key1, int n, F&& f) const {
+  // f(masked, first key, keys that are there, tile).  *odd is set where values were left out; returns the first key of the second loop
+  template <typename F> __device__ __forceinline__ int run(unsigned char* lds, int* odd, int key0, int key1, int n, F&& f) const {
     Part k, v;
-    auto store = [&](unsigned char* base, uint64_t there) __attribute__((always_inline)) {
-      if (there != ~0ull) clear(v, there);
+    auto store = [&](unsigned char* base, int j0, uint64_t there) __attribute__((always_inline)) {
+      if (there != ~0ull || j0 + 64 > n)
+        if (clear(v, there, lane)) *odd = 1;
       store_k(k, base);
       store_v(v, base + TILE);
     };
@@ -253,7 +281,9 @@ template <int HD, int NW, bool WIDE> struct TileLoader {
     load(k, kp, key0, id);
     load(v, vp, key0, id);
     id = pages(key0 + 64);
-    store(lds, there);
+    if (wave == 0 && lane == 0) *odd = 0;
+    __syncthreads();
+    store(lds, key0, there);
     __syncthreads();
     auto tiles = [&](auto masked) __attribute__((always_inline)) {
       for (; j0 < key1; j0 += 64, stage ^= 2 * TILE) {
@@ -267,12 +297,14 @@ template <int HD, int NW, bool WIDE> struct TileLoader {
         }
         f(masked, j0, there, (const unsigned char*)lds + stage);
         there = there_next;
-        if (more) store(lds + (stage ^ 2 * TILE), there);
+        if (more) store(lds + (stage ^ 2 * TILE), j0 + 64, there);
         __syncthreads();
       }
     };
     tiles(std::false_type{});
+    const int rest = j0;
     tiles(std::true_type{});
+    return rest;
   }
 };
 
@@ -360,42 +392,32 @@ template <int HD, int QB> struct Columns {
         for (int h = 0; h < 2; ++h)
           pf[qb].half[h] = pack4_bf16(p[qb][sub * 8 + 4 * h], p[qb][sub * 8 + 4 * h + 1], p[qb][sub * 8 + 4 * h + 2], p[qb][sub * 8 + 4 * h + 3]);
       const unsigned char* rows = v_rows + sub * 32 * HD * 2;
-      bool odd = false;
 #pragma unroll
       for (int eb = 0; eb < EB; ++eb) {
-        Frag vf = v_operand<HD>(rows, eb, r16, g);
-        if (MASKED) odd |= clear_odd(vf);
+        const Frag vf = v_operand<HD>(rows, eb, r16, g);
 #pragma unroll
         for (int qb = 0; qb < QB; ++qb) o[qb][eb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf.v, pf[qb].v, o[qb][eb], 0, 0, 0);
       }
-      if (MASKED && __any(odd)) add_odd<SUB>(p, sub, rows, r16, g);
     }
   }
-  // The values of 32 keys that are no numbers, to the columns that see them: rare, key by key
-  template <int SUB>
-  __device__ __forceinline__ void add_odd(const float (&p)[QB][8 * SUB], int sub, const unsigned char* rows, int r16, int g) {
+  // The values of keys j0 .. j1 - 1 that are no numbers, to the columns that see them: rare, key by key
+  __device__ __forceinline__ void add_odd_values(const AttnRows& a, const SeqSpan& sp, const PageView& in, int j0, int j1, int g) {
+    for (; j0 < j1; j0 += 64) {
+      uint64_t vis[QB];
+      const uint64_t there = in.there_at(j0);
+#pragma unroll
+      for (int qb = 0; qb < QB; ++qb) vis[qb] = seen_bits(mask_of(a, sp, row[qb]), sp, row[qb], j0, there);
 #pragma unroll 1
-    for (int key = 0; key < 32; ++key) {
-      float w[QB];
+      for (int k = 0; k < 64 && j0 + k < j1; ++k) {
+        if (!(there >> k & 1)) continue;
+        const char* values = in.value_row(j0 + k, HD) + g * 8;
 #pragma unroll
-      for (int qb = 0; qb < QB; ++qb) {
-        float mine = 0.f;
-#pragma unroll
-        for (int x = 0; x < 8; ++x) mine = (key & 7) == x ? p[qb][sub * 8 + x] : mine;
-        w[qb] = __shfl(mine, (key >> 3) * 16 + r16, 64);
-      }
-#pragma unroll
-      for (int eb = 0; eb < EB; ++eb) {
-        const uint2 four = *(const uint2*)(rows + key * (HD * 2) + v_place<HD>(key, eb) + g * 8);
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const uint32_t v = (i < 2 ? four.x : four.y) >> (i & 1) * 16 & 0xffffu;
-          if ((v & 0x7f80u) == 0x7f80u) {
+        for (int eb = 0; eb < EB; ++eb)
+          add_odd(values + eb * 32, [&](int i, float v) __attribute__((always_inline)) {
 #pragma unroll
             for (int qb = 0; qb < QB; ++qb)
-              if (w[qb] != 0.f) o[qb][eb][i] += w[qb] * __uint_as_float(v << 16);
-          }
-        }
+              if (vis[qb] >> k & 1) o[qb][eb][i] += v;
+          });
       }
     }
   }
@@ -479,9 +501,14 @@ struct Segment {
   int seq, hk, col_tile, key0, key1;
   bool whole;
   int place;                                 // of the partial result, if not whole
+  int first, parts, first_place;             // the workgroups that share the item: the first one, how many, the first one's place
+};
+// What a workgroup leaves for the join of each of its two places; parts 0: nothing
+struct PartNote {
+  int32_t seq, hk, col_tile, first, parts, first_place, pad[2];
 };
 __device__ __forceinline__ Segment segment_at(const Share& sh, const PagedRows& b, int64_t head_tiles, int64_t u, int64_t end, int64_t begin,
-                                              int workgroup, int lane) {
+                                              int64_t quota, int workgroup, int lane) {
   Segment s;
   s.hk = (int)(u / head_tiles);
   const int64_t at = u - s.hk * head_tiles;
@@ -497,6 +524,12 @@ __device__ __forceinline__ Segment segment_at(const Share& sh, const PagedRows& 
   s.key1 = (first + count) * 64 < sp.n + sp.count ? (first + count) * 64 : sp.n + sp.count;
   s.whole = count == tiles;
   s.place = workgroup * 2 + (u == begin ? 0 : 1);
+  if (!s.whole) {
+    const int64_t u0 = u - first;
+    s.first = (int)(u0 / quota);
+    s.parts = (int)((u0 + tiles - 1) / quota) - s.first + 1;
+    s.first_place = s.first * quota == u0 ? 0 : 1;
+  }
   return s;
 }
 __device__ __forceinline__ int shared_workgroup() {         // the number of this workgroup in the row
@@ -506,15 +539,16 @@ __device__ __forceinline__ int shared_workgroup() {         // the number of thi
 
 // The segments of this workgroup, one after the other
 template <int COLS, typename F>
-__device__ __forceinline__ void shared_items(Share& sh, const PagedRows& b, const AttnRows& a, int least, F&& item) {
+__device__ __forceinline__ void shared_items(Share& sh, const PagedRows& b, const AttnRows& a, int least, PartNote* notes, F&& item) {
   const int group = a.Hq / b.Hkv;
   const bool alone = b.seqs > kShareSeqs;                  // an item to a workgroup
-  int64_t head_tiles = 1, begin = 0, end = 1;
+  int64_t head_tiles = 1, begin = 0, end = 1, quota = 1;
   const int w = shared_workgroup();
+  bool noted[2] = {false, false};
   if (!alone) {
     head_tiles = uniform(share_out(sh, b, group, COLS));
-    if (!head_tiles) return;
-    const int64_t quota = quota_of(head_tiles, b.Hkv, gridDim.x, least), all = head_tiles * b.Hkv;
+    quota = quota_of(head_tiles, b.Hkv, gridDim.x, least);
+    const int64_t all = head_tiles * b.Hkv;
     begin = w * quota;
     end = begin + quota < all ? begin + quota : all;
   }
@@ -523,17 +557,22 @@ __device__ __forceinline__ void shared_items(Share& sh, const PagedRows& b, cons
     if (alone) {
       const SeqSpan sp = seq_span(b, blockIdx.z);
       if ((int)blockIdx.y * COLS >= sp.count * group) return;
-      s = Segment{(int)blockIdx.z, (int)blockIdx.x, (int)blockIdx.y, 0, sp.n + sp.count, true, 0};
+      s = Segment{(int)blockIdx.z, (int)blockIdx.x, (int)blockIdx.y, 0, sp.n + sp.count, true, 0, 0, 0, 0};
     } else {
-      s = segment_at(sh, b, head_tiles, u, end, begin, w, threadIdx.x & 63);
+      s = segment_at(sh, b, head_tiles, u, end, begin, quota, w, threadIdx.x & 63);
+      if (!s.whole) {
+        if (threadIdx.x == 0) notes[s.place] = PartNote{s.seq, s.hk, s.col_tile, s.first, s.parts, s.first_place, {0, 0}};
+        noted[s.place & 1] = true;
+      }
     }
     int lane = threadIdx.x & 63;
     asm volatile("" : "+v"(lane));                         // what an item works out from it is not kept from item to item
     item(s, lane);
-    u += (s.key1 - s.key0 + 63) / 64;
     if (alone) return;
+    u += (s.key1 - s.key0 + 63) / 64;
     __syncthreads();                                       // (the next one's tiles go where the last one's are read)
   }
+  if (!alone && threadIdx.x < 2 && !noted[threadIdx.x & 1]) notes[w * 2 + threadIdx.x].parts = 0;
 }
 
 }  // namespace
@@ -556,6 +595,7 @@ __global__ __launch_bounds__(256, 2) void paged_attn_few_kernel(PagedRows b, Att
   const int S = sp.n + sp.count, in_page = (1 << b.page_shift) - 1;
   const size_t page_elems = (size_t)b.Hkv * HD << b.page_shift, head_elems = (size_t)hk * HD << b.page_shift;
   const int32_t* table = b.table + (size_t)seq * b.table_width;
+  const PageView view(b, a, sp, seq, hk);
   const bf16_t *kp = (const bf16_t*)a.k_pages + head_elems, *vp = (const bf16_t*)a.v_pages + head_elems;
   unsigned char* v_rows = lds + wave * V_BYTES;
 
@@ -586,11 +626,19 @@ __global__ __launch_bounds__(256, 2) void paged_attn_few_kernel(PagedRows b, Att
       vr[i] = ((const Loose16*)(vp + page * page_elems + (size_t)row0 * HD + lane * 8))->v;
     }
   };
-  auto store_v = [&](uint32_t there) __attribute__((always_inline)) {
+  auto clear_v = [&](uint32_t there) __attribute__((always_inline)) {      // as TileLoader::clear
+    bool odd = false;
+#pragma unroll
+    for (int i = 0; i < LOADS; ++i) {
+      if (!(there >> (i * ROWS + lane / PIECES) & 1)) vr[i] = u32x4_t{0, 0, 0, 0};
+      odd |= tidy(vr[i]);
+    }
+    return __any(odd);
+  };
+  auto store_v = [&]() __attribute__((always_inline)) {
 #pragma unroll
     for (int i = 0; i < LOADS; ++i) {
       const int row = i * ROWS + lane / PIECES, piece = lane % PIECES;
-      if (there != 0xffffffffu && !(there >> row & 1)) vr[i] = u32x4_t{0, 0, 0, 0};
       *(u32x4_t*)(v_rows + row * (HD * 2) + v_place<HD>(row, piece >> 1) + (piece & 1) * 16) = vr[i];
     }
   };
@@ -615,15 +663,18 @@ __global__ __launch_bounds__(256, 2) void paged_attn_few_kernel(PagedRows b, Att
         const bool more = j0 + STEP < sl.key1;
         Frag kn[2][ES];
         if (more) load_k(kn, j0 + STEP, id_next);
-        store_v(MASKED ? there : 0xffffffffu);
+        bool odd = false;
+        if (MASKED) odd = clear_v(there);
+        store_v();
         if (more) load_v(j0 + STEP, id_next);
         uint64_t vis[QB] = {};
         if (MASKED) {
 #pragma unroll
-          for (int qb = 0; qb < QB; ++qb) vis[qb] = seen_bits(a, sp, cols.row[qb], j0, there);
+          for (int qb = 0; qb < QB; ++qb) vis[qb] = seen_bits(mask_of(a, sp, cols.row[qb]), sp, cols.row[qb], j0, there);
         }
         cols.template multiply<1, MASKED>([&](int, int bl, int es) __attribute__((always_inline)) { return kf[bl][es]; }, v_rows, vis,
                                           a.scale_log2, r16, g);
+        if (MASKED && odd) cols.add_odd_values(a, sp, view, j0, j0 + 32 < S ? j0 + 32 : S, g);
 #pragma unroll
         for (int bl = 0; bl < 2; ++bl)
 #pragma unroll
@@ -675,11 +726,13 @@ __global__ __launch_bounds__(256, 2) void paged_attn_few_kernel(PagedRows b, Att
 
 // More columns: every wavefront owns QB blocks of 16, tiles of 64 keys of K and V go through LDS for all of them.
 template <int HD, int QB, int NW>
-__global__ __launch_bounds__(64 * NW, 2) void paged_attn_tile_kernel(PagedRows b, AttnRows a, int least, float* part_o, float* part_ml) {
+__global__ __launch_bounds__(64 * NW, 2) void paged_attn_tile_kernel(PagedRows b, AttnRows a, int least, float* part_o, float* part_ml,
+                                                                    PartNote* notes) {
   using Cols = Columns<HD, QB>;
   constexpr int EB = Cols::EB, TILE = 64 * HD * 2, COLS = NW * QB * 16;
   __shared__ __attribute__((aligned(1024))) unsigned char lds[4 * TILE];   // two stages of (K tile, V tile)
   __shared__ Share sh;
+  __shared__ int odd;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), group = a.Hq / b.Hkv;
   auto item = [&](const Segment& s, int lane) __attribute__((always_inline)) {
     const int r16 = lane & 15, g = lane >> 4;
@@ -688,8 +741,8 @@ __global__ __launch_bounds__(64 * NW, 2) void paged_attn_tile_kernel(PagedRows b
     const bool works = col0 < sp.count * group;            // the others only bring tiles
     Cols cols;
     cols.start(a, sp, s.hk, group, col0, r16, g);
-    const TileLoader<HD, NW, false> in(b, a, sp, s.seq, s.hk, wave, lane);
-    in.run(lds, s.key0, s.key1, sp.n, [&](auto masked, int j0, uint64_t there, const unsigned char* base) __attribute__((always_inline)) {
+    const TileLoader<HD, NW> in(b, a, sp, s.seq, s.hk, wave, lane);
+    const int rest = in.run(lds, &odd, s.key0, s.key1, sp.n, [&](auto masked, int j0, uint64_t there, const unsigned char* base) __attribute__((always_inline)) {
       constexpr bool MASKED = decltype(masked)::value;
       if (!works) return;
       const int krow = 8 * (r16 >> 2) + (r16 & 3);
@@ -702,11 +755,12 @@ __global__ __launch_bounds__(64 * NW, 2) void paged_attn_tile_kernel(PagedRows b
       uint64_t vis[QB] = {};
       if (MASKED) {
 #pragma unroll
-        for (int qb = 0; qb < QB; ++qb) vis[qb] = seen_bits(a, sp, cols.row[qb], j0, there);
+        for (int qb = 0; qb < QB; ++qb) vis[qb] = seen_bits(mask_of(a, sp, cols.row[qb]), sp, cols.row[qb], j0, there);
       }
       cols.template multiply<2, MASKED>(k_of, base + TILE, vis, a.scale_log2, r16, g);
     });
     if (!works) return;
+    if (odd) cols.add_odd_values(a, sp, in, rest, s.key1, g);
 #pragma unroll
     for (int qb = 0; qb < QB; ++qb) {
       const float sum = sum_over_groups(cols.l[qb]);
@@ -721,7 +775,7 @@ __global__ __launch_bounds__(64 * NW, 2) void paged_attn_tile_kernel(PagedRows b
       }
     }
   };
-  shared_items<COLS>(sh, b, a, least, item);
+  shared_items<COLS>(sh, b, a, least, notes, item);
 }
 
 // Many columns: 32 to a wavefront, on the 32 x 32 x 16 instructions (half as many to issue, and a column lies in two lanes instead of
@@ -752,6 +806,11 @@ template <int HD> struct WideColumns {
       for (int x = 0; x < 16; ++x) o[eb][x] = 0.f;
   }
 
+  // The queries are waited for here, not at their first use inside the loop, where the wait would be for the tiles on their way too
+  __device__ __forceinline__ void arrived() {
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks) asm volatile("" : "+v"(q[ks].nat));
+  }
   // Scores of NB blocks of 32 keys
   template <int NB> __device__ __forceinline__ void scores(const unsigned char* k_rows, float (&p)[NB][16], int lane) const {
     const int r32 = lane & 31, half = lane >> 5;
@@ -836,7 +895,7 @@ template <int HD> struct WideColumns {
   template <int NB>
   __device__ __forceinline__ void advance(const unsigned char* v_rows, const unsigned char* k_rows, const Frag (&pf)[2 * NB], float (&p)[NB][16],
                                           int lane) {
-    constexpr int STEPS = 2 * KS * NB, AHEAD = 6;
+    constexpr int STEPS = 2 * KS * NB, AHEAD = 8;
     floatx16_t s[NB];
 #pragma unroll
     for (int kb = 0; kb < NB; ++kb)
@@ -863,217 +922,175 @@ template <int HD> struct WideColumns {
 #pragma unroll
       for (int x = 0; x < 16; ++x) p[kb][x] = s[kb][x];
   }
-  // Their values
-  template <bool MASKED, int NB> __device__ __forceinline__ void values(const unsigned char* v_rows, const Frag (&pf)[2 * NB], int lane) {
-    const int r32 = lane & 31, half = lane >> 5, r16 = lane & 15;
-#pragma unroll
-    for (int t = 0; t < 2 * NB; ++t) {                     // 16 keys
-      bool odd = false;
-#pragma unroll
-      for (int eb = 0; eb < EB; ++eb) {
-        Frag vf;
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {
-          const int row = 8 * half + 4 * h + (r16 >> 2);
-          const unsigned char* at = v_rows + (16 * t + row) * (HD * 2) + v_place<HD>(row, eb * 2 + ((lane >> 4) & 1)) + (r16 & 3) * 8;
-          const s16x4_t x = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4_t*)at);
-          vf.half[h] = *(const uint2*)&x;
-        }
-        if (MASKED) odd |= clear_odd(vf);
-        o[eb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf.v, pf[t].v, o[eb], 0, 0, 0);
-      }
-      if (MASKED && __any(odd)) {                          // the values that are no numbers, to the columns that see them
+  // The values of keys j0 .. j1 - 1 that are no numbers, to the columns that see them: rare, key by key
+  __device__ __forceinline__ void add_odd_values(const AttnRows& a, const SeqSpan& sp, const PageView& in, int j0, int j1, int half) {
+    for (; j0 < j1; j0 += 64) {
+      const uint64_t there = in.there_at(j0), vis = seen_bits(mask_of(a, sp, row), sp, row, j0, there);
 #pragma unroll 1
-        for (int key = 0; key < 16; ++key) {
-          uint32_t two = 0;
+      for (int k = 0; k < 64 && j0 + k < j1; ++k) {
+        if (!(there >> k & 1)) continue;
+        const char* values = in.value_row(j0 + k, HD) + half * 8;
 #pragma unroll
-          for (int x = 0; x < 4; ++x) two = (key >> 1 & 3) == x ? pf[t].u[x] : two;
-          const float w = __shfl(__uint_as_float(key & 1 ? two & 0xffff0000u : two << 16), (key >> 3) * 32 + r32, 64);
-#pragma unroll
-          for (int eb = 0; eb < EB; ++eb)
-#pragma unroll
-            for (int a4 = 0; a4 < 4; ++a4) {               // e = eb * 32 + 8 a4 + 4 half + i
-              const int unit = eb * 2 + (a4 >> 1);
-              const uint2 four = *(const uint2*)(v_rows + (16 * t + key) * (HD * 2) + v_place<HD>(key, unit) + (a4 & 1) * 16 + half * 8);
-#pragma unroll
-              for (int i = 0; i < 4; ++i) {
-                const uint32_t v = (i < 2 ? four.x : four.y) >> (i & 1) * 16 & 0xffffu;
-                if ((v & 0x7f80u) == 0x7f80u && w != 0.f) o[eb][a4 * 4 + i] += w * __uint_as_float(v << 16);
-              }
-            }
-        }
+        for (int x = 0; x < EB * 4; ++x)                   // e = eb * 32 + 8 a4 + 4 half + i
+          add_odd(values + x * 16, [&](int i, float v) __attribute__((always_inline)) {
+            if (vis >> k & 1) o[x >> 2][(x & 3) * 4 + i] += v;
+          });
       }
     }
   }
 };
 }  // namespace
 
-// CG column groups times KG key groups of wavefronts, eight: KG = 2 shares a tile's keys out where there are too few columns for eight.
-// The matrix units and the vector units of a SIMD work at the same time only if its two wavefronts (w and w + 4) are in different phases,
-// and wavefronts that meet at a barrier every tile are not.  So a tile has two phases, M (values of the tile before, scores of this
-// one) and V (softmax, loads and stores), with a barrier behind each, and the second four wavefronts are one phase behind the first.
-// In phases: K of tile t is read in 2t and 2t + 1, V of tile t in 2t + 2 and 2t + 3, so of two stages each, K of tile t + 1 and V of
-// tile t may be stored in 2t and 2t + 1: the first four store them in their V of tile t, the others in theirs of tile t - 1.
-template <int HD, int CG, int KG>
-__global__ __launch_bounds__(512, 2) void paged_attn_wide_kernel(PagedRows b, AttnRows a, int least, float* part_o, float* part_ml) {
-  using Cols = WideColumns<HD>;
-  using Loader = TileLoader<HD, 8, true>;
-  static_assert(CG * KG == 8, "eight wavefronts");
-  constexpr int EB = Cols::EB, TILE = 64 * HD * 2, NB = 2 / KG, COLS = CG * 32;
-  __shared__ __attribute__((aligned(1024))) unsigned char lds[4 * TILE];   // K, K, V, V
-  __shared__ Share sh;
-  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int cg = wave % CG, kg = wave / CG, late = wave >> 2, group = a.Hq / b.Hkv;
-  auto item = [&](const Segment& sl, int lane) __attribute__((always_inline)) {
-  const int half = lane >> 5;
-  const SeqSpan sp = seq_span(b, sl.seq);
-  const int seq = sl.seq, hk = sl.hk, wg_col0 = sl.col_tile * COLS;
-  const bool works = wg_col0 + cg * 32 < sp.count * group;                  // the others only bring tiles
-  const Loader in(b, a, sp, seq, hk, wave, lane);
-  const int tiles = (sl.key1 - sl.key0 + 63) / 64;
+// 64 x 16 bytes from `base` + off (a lane's own) to 1 KiB of LDS at `to`.  Written out because a read of LDS behind such a load, wherever it
+// goes, makes the compiler wait for it; this way the waits are those of wait_then_barrier.  The load writes no register.
+__device__ __forceinline__ void load_to_lds(const char* base, uint32_t off, uint32_t to) {
+  asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1" ::"v"(off), "s"(base), "s"(to) : "memory");
+}
+__device__ __forceinline__ void wait_then_barrier() { asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
+__device__ __forceinline__ uint32_t lds_address(const void* p) { return (uint32_t)(uintptr_t)(__attribute__((address_space(3))) const void*)p; }
 
-  // pages of tiles s .. s + 2 (s: the tile whose values are asked for next)
-  int id[3][Loader::LOADS];
-  auto pages = [&](int (&x)[Loader::LOADS], int tile) __attribute__((always_inline)) {
+// Four wavefronts, two workgroups to a compute unit.  A tile has two halves: the softmax (vector units), and the values of the tile with
+// the scores of the next (matrix units, operands from LDS); the other workgroup is somewhere else in its tiles, so both kinds of unit
+// have work.  K and V come straight to LDS, two stages of each, asked for behind barrier t (K of tile t + 2 and V of t + 1, where K of t and
+// V of t - 1 were: read in front of it) and waited for in front of barrier t + 1.
+template <int HD>
+__global__ __launch_bounds__(256, 2) void paged_attn_wide_kernel(PagedRows b, AttnRows a, int least, float* part_o, float* part_ml, PartNote* notes) {
+  using Cols = WideColumns<HD>;
+  constexpr int EB = Cols::EB, TILE = 64 * HD * 2, COLS = 128, PIECES = HD / 8, ROWS = 64 / PIECES, PASS = 4 * ROWS, LOADS = 64 / PASS;
+  __shared__ __attribute__((aligned(1024))) unsigned char lds[4 * TILE];   // K, K, V, V
+  __shared__ uint64_t masks[COLS][kMaskWords];                             // of the item's rows
+  __shared__ Share sh;
+  __shared__ int odd;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), group = a.Hq / b.Hkv;
+  auto item = [&](const Segment& sl, int lane) __attribute__((always_inline)) {
+    const int half = lane >> 5;
+    const SeqSpan sp = seq_span(b, sl.seq);
+    const int wg_col0 = sl.col_tile * COLS;
+    const bool works = wg_col0 + wave * 32 < sp.count * group;             // the others only bring tiles
+    const PageView in(b, a, sp, sl.seq, sl.hk);
+    const int tiles = (sl.key1 - sl.key0 + 63) / 64;
+
+    // load i of a tile: rows i * PASS + wave * ROWS on, the lane's piece of its row where the swizzle wants it
+    const int my_row = lane / PIECES, at = lane % PIECES;
+    const uint32_t k_off = my_row * (HD * 2) + (wide_k_place<HD>(wave * ROWS + my_row, at));
+    const uint32_t v_off = my_row * (HD * 2) + v_place<HD>(wave * ROWS + my_row, at >> 1) + (at & 1) * 16;
+    const uint32_t lds0 = lds_address(lds) + wave * 1024;
+    auto pages = [&](int (&x)[LOADS], int tile) __attribute__((always_inline)) {
 #pragma unroll
-    for (int i = 0; i < Loader::LOADS; ++i) x[i] = in.page_at(sl.key0 + 64 * tile + i * Loader::PASS + wave * Loader::ROWS);
-  };
-#pragma unroll
-  for (int d = 0; d < 3; ++d) pages(id[d], d);
-  typename Loader::Part k0, v0, k1, v1;
-  in.load(k0, in.kp, sl.key0, id[0]);
-  Cols cols;
-  cols.start(a, sp, hk, group, wg_col0 + cg * 32 + (lane & 31), half);
-  // tiles in front that every column sees whole
-  int whole = (sp.n - sl.key0) / 64;
-  whole = whole < 0 ? 0 : whole > tiles ? tiles : whole;
-  for (int i = 0; i < whole; i += 64) {                    // a lane a tile
-    bool bad = false;
-    if (i + lane < whole)
-      for (int r = 0; r < 64; r += 1 << (in.shift < 6 ? in.shift : 6))
-        bad |= (unsigned)in.table[(sl.key0 + 64 * (i + lane) + r) >> in.shift] >= (unsigned)in.n_pages;
-    const uint64_t any = __ballot(bad);
-    if (any) whole = i + __builtin_ctzll(any);
-  }
-  int next = 0;                                            // s
-  auto ask = [&](typename Loader::Part& k, typename Loader::Part& v) __attribute__((always_inline)) {
-    if (next < tiles) in.load(v, in.vp, sl.key0 + 64 * next, id[0]);
-    if (next + 1 < tiles) in.load(k, in.kp, sl.key0 + 64 * (next + 1), id[1]);
-#pragma unroll
-    for (int i = 0; i < Loader::LOADS; ++i) id[0][i] = id[1][i], id[1][i] = id[2][i];
-    pages(id[2], next + 3);
-    ++next;
-  };
-  auto store = [&](typename Loader::Part& k, typename Loader::Part& v, int s) __attribute__((always_inline)) {
-    if (s >= whole && s < tiles) in.clear(v, in.there_of(sl.key0 + 64 * s, in.pages(sl.key0 + 64 * s)));
-    if (s + 1 < tiles) in.store_k(k, lds + ((s + 1) & 1) * TILE);
-    if (s < tiles) in.store_v(v, lds + 2 * TILE + (s & 1) * TILE);
-  };
-  in.store_k(k0, lds);
-  if (late) {
-    ask(k1, v1);
-    ask(k0, v0);
-  } else {
-    ask(k0, v0);
-    ask(k1, v1);
-  }
-  __syncthreads();
-  if (late) {
-    store(k1, v1, 0);
-    ask(k1, v1);
-    __syncthreads();
-  }
-  float p[NB][16];
-  Frag pf[2 * NB];
-  const int first = NB == 1 ? kg * 32 * HD * 2 : 0;
-  if (works) cols.template scores<NB>(lds + first, p, lane);
-  __syncthreads();
-  auto step = [&](auto masked, int t, typename Loader::Part& k, typename Loader::Part& v) __attribute__((always_inline)) {
-    constexpr bool MASKED = decltype(masked)::value;
-    if (works) {
-      uint64_t vis = 0;
-      if (MASKED) {
-        const int j0 = sl.key0 + 64 * t;
-        vis = seen_bits(a, sp, cols.row, j0, in.there_of(j0, in.pages(j0))) >> (NB == 1 ? 32 * kg : 0);
+      for (int i = 0; i < LOADS; ++i) {
+        const int id = in.page_at(sl.key0 + 64 * tile + i * PASS + wave * ROWS);
+        x[i] = (unsigned)id < (unsigned)in.n_pages ? id : 0;
       }
-      cols.template soften<MASKED, NB>(p, pf, vis, a.scale_log2, lane);
+    };
+    auto ask = [&](const char* pool, uint32_t off, int tile, const int (&id)[LOADS], uint32_t to) __attribute__((always_inline)) {
+#pragma unroll
+      for (int i = 0; i < LOADS; ++i) {
+        const int slot = sl.key0 + 64 * tile + i * PASS + wave * ROWS;
+        load_to_lds(pool + id[i] * in.page_bytes + (size_t)(slot & ((1 << in.shift) - 1)) * (HD * 2), off, to + i * 4096);
+      }
+    };
+    int id1[LOADS], id2[LOADS];                            // pages of tiles t + 1, t + 2
+    {
+      int id0[LOADS];
+      pages(id0, 0);
+      pages(id1, 1);
+      pages(id2, 2);
+      ask(in.kp, k_off, 0, id0, lds0);
+      if (tiles > 1) ask(in.kp, k_off, 1, id1, lds0 + TILE);
+      ask(in.vp, v_off, 0, id0, lds0 + 2 * TILE);
     }
-    store(k, v, t + late);
-    ask(k, v);
-    __syncthreads();
-    if (works && !MASKED) {                                // (scores of a tile past the slice's last are nobody's)
-      cols.template advance<NB>(lds + 2 * TILE + (t & 1) * TILE + first, lds + ((t + 1) & 1) * TILE + first, pf, p, lane);
-    } else if (works) {
-      cols.template values<MASKED, NB>(lds + 2 * TILE + (t & 1) * TILE + first, pf, lane);
-      if (t + 1 < tiles) cols.template scores<NB>(lds + ((t + 1) & 1) * TILE + first, p, lane);
+    Cols cols;
+    cols.start(a, sp, sl.hk, group, wg_col0 + wave * 32 + (lane & 31), half);
+    const int row0 = wg_col0 / group;
+    if (a.anc && sl.key1 > sp.n) {
+      const int rows = sp.count - row0 < COLS ? sp.count - row0 : COLS;
+      for (int i = wave * 64 + lane; i < rows * kMaskWords; i += 256) masks[i / kMaskWords][i % kMaskWords] = a.anc[(size_t)(sp.row0 + row0) * kMaskWords + i];
     }
-    __syncthreads();
+    if (threadIdx.x == 0) odd = 0;
+    // tiles in front that every column sees whole, and whether a page is missing
+    int whole = sp.n > sl.key0 ? (sp.n - sl.key0) / 64 : 0;
+    whole = whole < tiles ? whole : tiles;
+    bool missing = false;
+    for (int i = 0; i < tiles; i += 64) {                  // a lane a tile
+      bool bad = false;
+      if (i + lane < tiles)
+        for (int r = 0; r < 64; r += 1 << (in.shift < 6 ? in.shift : 6)) {
+          const int slot = sl.key0 + 64 * (i + lane) + r;
+          bad |= (unsigned)in.table[(slot < in.S ? slot : in.S - 1) >> in.shift] >= (unsigned)in.n_pages;
+        }
+      const uint64_t any = __ballot(bad);
+      if (any) {
+        const int first = i + __builtin_ctzll(any);
+        whole = first < whole ? first : whole;
+        missing = true;
+        break;
+      }
+    }
+    cols.arrived();
+    wait_then_barrier();
+    float p[2][16];
+    Frag pf[4];
+    if (works) cols.template scores<2>(lds, p, lane);
+    auto step = [&](auto masked, int t) __attribute__((always_inline)) {
+      constexpr bool MASKED = decltype(masked)::value;
+      const int j0 = sl.key0 + 64 * t;
+      const uint64_t there = !MASKED ? ~0ull : missing ? in.there_at(j0) : in.up_to_end(j0);
+      if (works) {
+        uint64_t vis = 0;
+        if (MASKED) vis = seen_bits(a.anc ? masks[cols.row < sp.count ? cols.row - row0 : 0] : nullptr, sp, cols.row, j0, there);
+        cols.template soften<MASKED, 2>(p, pf, vis, a.scale_log2, lane);
+      }
+      wait_then_barrier();
+      if (t + 2 < tiles) ask(in.kp, k_off, t + 2, id2, lds0 + (t & 1) * TILE);
+      if (t + 1 < tiles) ask(in.vp, v_off, t + 1, id1, lds0 + (2 + ((t + 1) & 1)) * TILE);
+#pragma unroll
+      for (int i = 0; i < LOADS; ++i) id1[i] = id2[i];
+      pages(id2, t + 3);
+      unsigned char* v_rows = lds + (2 + (t & 1)) * TILE;
+      if (MASKED) {
+        // values of keys that are not there become 0 (0 times what lies there is no 0), and those that are no numbers, for add_odd
+#pragma unroll
+        for (int i = 0; i < LOADS; ++i) {
+          u32x4_t* at_lds = (u32x4_t*)(v_rows + i * 4096 + wave * 1024 + lane * 16);
+          u32x4_t x = *at_lds;
+          if (!(there >> (i * PASS + wave * ROWS + lane / PIECES) & 1)) x = u32x4_t{0, 0, 0, 0};
+          if (tidy(x)) odd = 1;
+          *at_lds = x;
+        }
+        __syncthreads();
+      }
+      // (scores of a tile past the slice's last are nobody's)
+      if (works) cols.template advance<2>(v_rows, lds + ((t + 1) & 1) * TILE, pf, p, lane);
+    };
+    int t = 0;
+    for (; t < whole; ++t) step(std::false_type{}, t);
+    for (; t < tiles; ++t) step(std::true_type{}, t);
+    if (works && odd) cols.add_odd_values(a, sp, in, sl.key0 + 64 * whole, sl.key1, half);
+
+    if (!works) return;
+    auto sw = __builtin_amdgcn_permlane32_swap(__float_as_uint(cols.l), __float_as_uint(cols.l), false, false);
+    const float sum = __uint_as_float(sw[0]) + __uint_as_float(sw[1]);
+    if (!sl.whole) {
+      const size_t column = (size_t)sl.place * COLS + wave * 32 + (lane & 31);
+      float* po = part_o + column * HD + half * 4;
+#pragma unroll
+      for (int eb = 0; eb < EB; ++eb)
+#pragma unroll
+        for (int a4 = 0; a4 < 4; ++a4)
+          *(float4*)(po + eb * 32 + a4 * 8) = make_float4(cols.o[eb][a4 * 4], cols.o[eb][a4 * 4 + 1], cols.o[eb][a4 * 4 + 2], cols.o[eb][a4 * 4 + 3]);
+      if (half == 0) *(float2*)(part_ml + column * 2) = make_float2(cols.m, sum);
+    } else if (cols.row < sp.count) {
+      const float inv = sum == 0.f ? 0.f : 1.0f / sum;
+      bf16_t* out = (bf16_t*)a.out + (int64_t)(sp.row0 + cols.row) * a.out_stride + (int64_t)cols.head * HD + half * 4;
+#pragma unroll
+      for (int eb = 0; eb < EB; ++eb)
+#pragma unroll
+        for (int a4 = 0; a4 < 4; ++a4)
+          ((Loose8*)(out + eb * 32 + a4 * 8))->v = sum == 0.f ? make_uint2(0, 0) :
+              pack4_bf16(cols.o[eb][a4 * 4] * inv, cols.o[eb][a4 * 4 + 1] * inv, cols.o[eb][a4 * 4 + 2] * inv, cols.o[eb][a4 * 4 + 3] * inv);
+    }
   };
-  int t = 0;
-  for (; t + 2 <= whole; t += 2) {
-    step(std::false_type{}, t, k0, v0);
-    step(std::false_type{}, t + 1, k1, v1);
-  }
-  for (; t < tiles; ++t) {                                 // (t is even at first: the sets change places from step to step)
-    step(std::true_type{}, t, k0, v0);
-#pragma unroll
-    for (int i = 0; i < Loader::LOADS; ++i) {
-      const u32x4_t x = k0[i], y = v0[i];
-      k0[i] = k1[i], v0[i] = v1[i], k1[i] = x, v1[i] = y;
-    }
-  }
-  if (!late) __syncthreads();
-  auto sw = __builtin_amdgcn_permlane32_swap(__float_as_uint(cols.l), __float_as_uint(cols.l), false, false);
-  float sum = __uint_as_float(sw[0]) + __uint_as_float(sw[1]);
-  if constexpr (KG == 2) {                                 // (behind the last tile's barrier: its LDS is free)
-    float2* lds_ml = (float2*)lds;
-    lds_ml[(kg * CG + cg) * 64 + lane] = make_float2(cols.m, sum);
-    __syncthreads();
-    const float2 ml = lds_ml[((1 - kg) * CG + cg) * 64 + lane];
-    __syncthreads();
-    const float all = fmaxf(cols.m, ml.x), ref = all == -INFINITY ? 0.f : all;
-    const float mine = __builtin_amdgcn_exp2f(cols.m - ref);
-    sum = sum * mine + ml.y * __builtin_amdgcn_exp2f(ml.x - ref);
-    cols.m = all;
-#pragma unroll
-    for (int eb = 0; eb < EB; ++eb) cols.o[eb] *= mine;
-    floatx4_t* lds_o = (floatx4_t*)lds + cg * 64 * EB * 4;
-    if (works && kg) {
-#pragma unroll
-      for (int x = 0; x < EB * 4; ++x)
-        lds_o[x * 64 + lane] = floatx4_t{cols.o[x >> 2][(x & 3) * 4], cols.o[x >> 2][(x & 3) * 4 + 1], cols.o[x >> 2][(x & 3) * 4 + 2], cols.o[x >> 2][(x & 3) * 4 + 3]};
-    }
-    __syncthreads();
-    if (kg) return;
-#pragma unroll
-    for (int x = 0; x < EB * 4; ++x) {
-      const floatx4_t y = lds_o[x * 64 + lane];
-#pragma unroll
-      for (int i = 0; i < 4; ++i) cols.o[x >> 2][(x & 3) * 4 + i] += y[i];
-    }
-  }
-  if (!works) return;
-  if (!sl.whole) {
-    const size_t at = (size_t)sl.place * COLS + cg * 32 + (lane & 31);
-    float* po = part_o + at * HD + half * 4;
-#pragma unroll
-    for (int eb = 0; eb < EB; ++eb)
-#pragma unroll
-      for (int a4 = 0; a4 < 4; ++a4)
-        *(float4*)(po + eb * 32 + a4 * 8) = make_float4(cols.o[eb][a4 * 4], cols.o[eb][a4 * 4 + 1], cols.o[eb][a4 * 4 + 2], cols.o[eb][a4 * 4 + 3]);
-    if (half == 0) *(float2*)(part_ml + at * 2) = make_float2(cols.m, sum);
-  } else if (cols.row < sp.count) {
-    const float inv = sum == 0.f ? 0.f : 1.0f / sum;
-    bf16_t* out = (bf16_t*)a.out + (int64_t)(sp.row0 + cols.row) * a.out_stride + (int64_t)cols.head * HD + half * 4;
-#pragma unroll
-    for (int eb = 0; eb < EB; ++eb)
-#pragma unroll
-      for (int a4 = 0; a4 < 4; ++a4)
-        ((Loose8*)(out + eb * 32 + a4 * 8))->v = sum == 0.f ? make_uint2(0, 0) :
-            pack4_bf16(cols.o[eb][a4 * 4] * inv, cols.o[eb][a4 * 4 + 1] * inv, cols.o[eb][a4 * 4 + 2] * inv, cols.o[eb][a4 * 4 + 3] * inv);
-  }
-  };
-  shared_items<COLS>(sh, b, a, least, item);
+  shared_items<COLS>(sh, b, a, least, notes, item);
 }
 
 // out = sum_s 2^(m_s - m) O_s / sum_s 2^(m_s - m) l_s over the slices of a sequence, in a fixed order.  A workgroup per (row, head) and
@@ -1137,50 +1154,73 @@ __global__ __launch_bounds__(PARTS * (HD / 4)) void paged_attn_join_kernel(Paged
       sum == 0.f ? make_uint2(0, 0) : pack4_bf16(acc[0] * inv, acc[1] * inv, acc[2] * inv, acc[3] * inv);
 }
 
-// The same for shared-out work: the partial results of an item, workgroup after workgroup.  A workgroup of 256 threads per row and 256 /
-// (HD / 4) query heads.
+// The same for shared-out work.  A workgroup per place; those that hold a part of an item share the item's elements out among them, four
+// elements to a unit, and where that leaves fewer units than threads, the threads share the parts.
 template <int HD, int COLS>
-__global__ __launch_bounds__(256) void paged_attn_share_join_kernel(PagedRows b, AttnRows a, int workgroups, int least, const float* part_o,
-                                                                   const float* part_ml) {
-  __shared__ Share sh;
-  constexpr int T = HD / 4;
-  const int seq = blockIdx.z, row = blockIdx.y, head = blockIdx.x * (256 / T) + threadIdx.x / T, e = threadIdx.x % T * 4;
-  const SeqSpan sp = seq_span(b, seq);
-  if (row >= sp.count) return;
-  const int group = a.Hq / b.Hkv;
-  const int64_t head_tiles = share_out(sh, b, group, COLS);
-  if (head >= a.Hq) return;
-  const int64_t quota = quota_of(head_tiles, b.Hkv, workgroups, least);
-  const int tiles = (sp.n + sp.count + 63) / 64, hk = head / group, col = row * group + head % group;
-  const int64_t u0 = hk * head_tiles + sh.before[seq] + (int64_t)(col / COLS) * tiles, w0 = u0 / quota, w1 = (u0 + tiles - 1) / quota;
-  if (w0 == w1) return;                                    // one workgroup had it whole
-  auto place = [&](int64_t w) { return (size_t)(w * 2 + (w * quota >= u0 ? 0 : 1)) * COLS + col % COLS; };
-  float top = -INFINITY, sum = 0.f;
-  floatx4_t acc = floatx4_t{0.f, 0.f, 0.f, 0.f};
-  constexpr int NS = 4;                                    // requested at a time
-  for (int64_t w = w0; w <= w1; w += NS) {
-    float2 ml[NS];
-    floatx4_t x[NS];
+__global__ __launch_bounds__(256) void paged_attn_share_join_kernel(PagedRows b, AttnRows a, const float* part_o, const float* part_ml,
+                                                                   const PartNote* notes) {
+  const PartNote n = notes[blockIdx.x];
+  if (!n.parts) return;
+  constexpr int T = HD / 4, UNITS = COLS * T;
+  const SeqSpan sp = seq_span(b, n.seq);
+  const int tid = threadIdx.x, group = a.Hq / b.Hkv, mine = (int)(blockIdx.x >> 1) - n.first;
+  int lo, hi;
+  even_share(UNITS, n.parts, mine, lo, hi);
+  int width = 256, groups = 1;                             // units and shares of the parts at a time
+  while (width / 2 >= hi - lo && width > 8) width /= 2, groups *= 2;
+  const int share = tid / width;
+  __shared__ floatx4_t lds_o[256];
+  __shared__ float2 lds_ml[256];
+  auto place = [&](int part) { return (size_t)((n.first + part) * 2 + (part ? 0 : n.first_place)) * COLS; };
+  for (int u0 = lo; u0 < hi; u0 += width) {
+    const int unit = u0 + tid % width, col = unit / T, e = unit % T * 4, c = n.col_tile * COLS + col, row = c / group;
+    const bool in = unit < hi && row < sp.count;
+    float top = -INFINITY, sum = 0.f;
+    floatx4_t acc = floatx4_t{0.f, 0.f, 0.f, 0.f};
+    constexpr int NS = 4;                                  // requested at a time
+    if (in)
+      for (int p0 = share; p0 < n.parts; p0 += NS * groups) {
+        float2 ml[NS];
+        floatx4_t x[NS];
 #pragma unroll
-    for (int i = 0; i < NS; ++i) {
-      const size_t at = place(w + i <= w1 ? w + i : w);
-      ml[i] = *(const float2*)(part_ml + at * 2);
-      x[i] = *(const floatx4_t*)(part_o + at * HD + e);
+        for (int i = 0; i < NS; ++i) {
+          const size_t at = place(p0 + i * groups < n.parts ? p0 + i * groups : p0) + col;
+          ml[i] = *(const float2*)(part_ml + at * 2);
+          x[i] = *(const floatx4_t*)(part_o + at * HD + e);
+        }
+#pragma unroll
+        for (int i = 0; i < NS; ++i) {
+          if (p0 + i * groups >= n.parts) break;
+          const float now = fmaxf(top, ml[i].x), ref = now == -INFINITY ? 0.f : now;
+          const float old = __builtin_amdgcn_exp2f(top - ref), f = __builtin_amdgcn_exp2f(ml[i].x - ref);
+          sum = fmaf(f, ml[i].y, sum * old);
+#pragma unroll
+          for (int k = 0; k < 4; ++k) acc[k] = fmaf(f, x[i][k], acc[k] * old);
+          top = now;
+        }
+      }
+    if (groups > 1) {
+      __syncthreads();
+      lds_o[tid] = acc;
+      lds_ml[tid] = make_float2(top, sum);
+      __syncthreads();
+      if (share == 0)
+        for (int i = 1; i < groups; ++i) {
+          const float2 ml = lds_ml[tid + i * width];
+          const floatx4_t x = lds_o[tid + i * width];
+          const float now = fmaxf(top, ml.x), ref = now == -INFINITY ? 0.f : now;
+          const float old = __builtin_amdgcn_exp2f(top - ref), f = __builtin_amdgcn_exp2f(ml.x - ref);
+          sum = fmaf(f, ml.y, sum * old);
+#pragma unroll
+          for (int k = 0; k < 4; ++k) acc[k] = fmaf(f, x[k], acc[k] * old);
+          top = now;
+        }
     }
-#pragma unroll
-    for (int i = 0; i < NS; ++i) {
-      if (w + i > w1) break;
-      const float now = fmaxf(top, ml[i].x), ref = now == -INFINITY ? 0.f : now;
-      const float old = __builtin_amdgcn_exp2f(top - ref), f = __builtin_amdgcn_exp2f(ml[i].x - ref);
-      sum = fmaf(f, ml[i].y, sum * old);
-#pragma unroll
-      for (int c = 0; c < 4; ++c) acc[c] = fmaf(f, x[i][c], acc[c] * old);
-      top = now;
-    }
+    if (!in || share) continue;
+    const float inv = sum == 0.f ? 0.f : 1.0f / sum;
+    ((Loose8*)((bf16_t*)a.out + (int64_t)(sp.row0 + row) * a.out_stride + (int64_t)(n.hk * group + c % group) * HD + e))->v =
+        sum == 0.f ? make_uint2(0, 0) : pack4_bf16(acc[0] * inv, acc[1] * inv, acc[2] * inv, acc[3] * inv);
   }
-  const float inv = sum == 0.f ? 0.f : 1.0f / sum;
-  ((Loose8*)((bf16_t*)a.out + (int64_t)(sp.row0 + row) * a.out_stride + (int64_t)head * HD + e))->v =
-      sum == 0.f ? make_uint2(0, 0) : pack4_bf16(acc[0] * inv, acc[1] * inv, acc[2] * inv, acc[3] * inv);
 }
 
 namespace {
@@ -1209,10 +1249,10 @@ AttnPlan attn_plan(int dtype, const PagedRows& b, int Hq) {
     p.splits = (S + p.split_len - 1) / p.split_len;
     return p;
   }
-  p.cols = cols <= 64 ? 64 : cols <= 128 ? 128 : 256;
+  p.cols = cols <= 64 ? 64 : 128;
   p.least = 4;
   const int64_t most = (int64_t)b.seqs * b.Hkv * ((cols + p.cols - 1) / p.cols) * ((S + 63) / 64);        // tiles
-  p.workgroups = b.seqs > kShareSeqs ? 0 : p.cols == 64 ? 512 : 256;
+  p.workgroups = b.seqs > kShareSeqs ? 0 : 512;
   if (p.workgroups > (most + p.least - 1) / p.least) p.workgroups = (int)((most + p.least - 1) / p.least);
   return p;
 }
@@ -1221,7 +1261,8 @@ size_t part_columns(const AttnPlan& p, const PagedRows& b, int Hq) {        // c
   if (p.few) return p.splits > 1 ? (size_t)p.splits * b.rows * Hq : 0;
   return (size_t)p.workgroups * 2 * p.cols;
 }
-template <int HD> hipError_t launch_attn_hd(const AttnPlan& p, const PagedRows& b, const AttnRows& a, float* part_o, float* part_ml, hipStream_t s) {
+template <int HD>
+hipError_t launch_attn_hd(const AttnPlan& p, const PagedRows& b, const AttnRows& a, float* part_o, float* part_ml, PartNote* notes, hipStream_t s) {
   if (p.few) {
     auto f = p.blocks == 1 ? paged_attn_few_kernel<HD, 1> : paged_attn_few_kernel<HD, 2>;
     hipLaunchKernelGGL(f, dim3(b.Hkv, p.splits, b.seqs), dim3(256), 0, s, b, a, p.split_len, part_o, part_ml);
@@ -1234,19 +1275,19 @@ template <int HD> hipError_t launch_attn_hd(const AttnPlan& p, const PagedRows& 
   }
   const int cols = b.max_rows * (a.Hq / b.Hkv);
   const dim3 grid = p.workgroups ? dim3(p.workgroups) : dim3(b.Hkv, (cols + p.cols - 1) / p.cols, b.seqs);
-  auto f = p.cols == 64 ? paged_attn_tile_kernel<HD, 1, 4> : p.cols == 128 ? paged_attn_wide_kernel<HD, 4, 2> : paged_attn_wide_kernel<HD, 8, 1>;
-  hipLaunchKernelGGL(f, grid, dim3(p.cols == 64 ? 256 : 512), 0, s, b, a, p.least, part_o, part_ml);
+  auto f = p.cols == 64 ? paged_attn_tile_kernel<HD, 1, 4> : paged_attn_wide_kernel<HD>;
+  hipLaunchKernelGGL(f, grid, dim3(256), 0, s, b, a, p.least, part_o, part_ml, notes);
   if (p.workgroups > 1) {
-    auto j = p.cols == 64 ? paged_attn_share_join_kernel<HD, 64> : p.cols == 128 ? paged_attn_share_join_kernel<HD, 128> : paged_attn_share_join_kernel<HD, 256>;
-    constexpr int heads = 256 / (HD / 4);
-    hipLaunchKernelGGL(j, dim3((a.Hq + heads - 1) / heads, b.max_rows, b.seqs), dim3(256), 0, s, b, a, p.workgroups, p.least, part_o, part_ml);
+    auto j = p.cols == 64 ? paged_attn_share_join_kernel<HD, 64> : paged_attn_share_join_kernel<HD, 128>;
+    hipLaunchKernelGGL(j, dim3(p.workgroups * 2), dim3(256), 0, s, b, a, part_o, part_ml, notes);
   }
   return hipGetLastError();
 }
 }  // namespace
 
 size_t paged_attn_scratch_bytes(int dtype, const PagedRows& b, int Hq) {
-  return part_columns(attn_plan(dtype, b, Hq), b, Hq) * (b.hd + 2) * sizeof(float);
+  const AttnPlan p = attn_plan(dtype, b, Hq);
+  return part_columns(p, b, Hq) * (b.hd + 2) * sizeof(float) + (size_t)p.workgroups * 2 * sizeof(PartNote);
 }
 
 hipError_t launch_paged_attn(int dtype, const PagedRows& b, const AttnRows& a, void* scratch, hipStream_t s) {
@@ -1259,7 +1300,8 @@ hipError_t launch_paged_attn(int dtype, const PagedRows& b, const AttnRows& a, v
   }
   float* part_o = (float*)scratch;
   float* part_ml = part_o + part_columns(p, b, a.Hq) * b.hd;
-  return b.hd == 64 ? launch_attn_hd<64>(p, b, a, part_o, part_ml, s) : launch_attn_hd<128>(p, b, a, part_o, part_ml, s);
+  PartNote* notes = (PartNote*)(part_ml + part_columns(p, b, a.Hq) * 2);
+  return b.hd == 64 ? launch_attn_hd<64>(p, b, a, part_o, part_ml, notes, s) : launch_attn_hd<128>(p, b, a, part_o, part_ml, notes, s);
 }
 
 }  // namespace ht
