@@ -451,128 +451,101 @@ __device__ __forceinline__ Slice slice_of(const SeqSpan& sp, int split, int spli
   return Slice{k0, k0 + split_len < S ? k0 + split_len : S, count};
 }
 
-// Shared-out work of the kernels for many columns.  The tiles of all (head, sequence, column tile) items stand in one row, heads outermost
-// and the tiles of an item innermost, and every workgroup takes the next `quota` of them: lengths may be as ragged as they like.  An
-// item that several workgroups share leaves partial results, two places to a workgroup (an item is a workgroup's first, and keeps its place
-// 0, or its last, place 1; those between are whole).  Workgroups of one XCD (numbers that are equal modulo 8) stand next to each other:
-// column tiles of the same keys meet in one L2.
-constexpr int kShareSeqs = 256;              // sequences whose tiles a workgroup can add up (a thread each)
-struct Share {
-  int64_t before[kShareSeqs + 1];            // tiles of a head in front of sequence i
-  int64_t part[8];
+// Shared-out work of the kernels for many columns.  An item is a (head, sequence, column tile); a long one is cut into parts, a workgroup
+// each, none of more than T tiles with kItemTiles for what starting and ending costs, T the smallest with which all parts fit the
+// grid: lengths may be as ragged as they like.  The parts of an item leave partial results, which a second kernel joins.  Every
+// wavefront works this out for itself.  Workgroups of one XCD (numbers that are equal modulo 8) have consecutive parts, heads
+// outermost: column tiles of the same keys meet in one L2.
+constexpr int kShareSeqs = 256;              // sequences that a wavefront can add up
+constexpr int kItemTiles = 3;                // 5 to 6 us of a workgroup; a tile 1.9
+struct Part {
+  int seq, hk, col_tile, key0, key1;
+  int parts, part, place;                    // of the item: how many, which, and where in the row of parts this one stands
 };
-__device__ __forceinline__ int64_t tiles_of(const SeqSpan& sp, int group, int cols) {
-  return sp.count ? (int64_t)((sp.n + sp.count + 63) / 64) * ((sp.count * group + cols - 1) / cols) : 0;
+// What a workgroup leaves for the join; parts 0: nothing, 1: a whole item
+struct PartNote {
+  int32_t seq, hk, col_tile, part, parts, pad[3];
+};
+__device__ __forceinline__ int wave_total(int v) {
+#pragma unroll
+  for (int o = 32; o; o >>= 1) v += __shfl_xor(v, o, 64);
+  return __builtin_amdgcn_readfirstlane(v);
 }
-// Fills `sh`; the tiles of a head.  All threads of the workgroup, 256 or more.
-__device__ __forceinline__ int64_t share_out(Share& sh, const PagedRows& b, int group, int cols) {
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-  const int64_t mine = tid < b.seqs && tid < kShareSeqs ? tiles_of(seq_span(b, tid), group, cols) : 0;
-  int64_t run = mine;
+// False: nothing for this workgroup
+__device__ __forceinline__ bool part_of_workgroup(const PagedRows& b, int group, int cols, int least, Part& out) {
+  constexpr int PER = kShareSeqs / 64;
+  const int lane = threadIdx.x & 63;
+  if (!least) {                                            // an item to a workgroup
+    const SeqSpan sp = seq_span(b, blockIdx.z);
+    out = Part{(int)blockIdx.z, (int)blockIdx.x, (int)blockIdx.y, 0, sp.n + sp.count, 1, 0, 0};
+    return (int)blockIdx.y * cols < sp.count * group;
+  }
+  int tiles[PER], items[PER], total = 0, longest = 0;      // of sequences PER lane .. + PER - 1
+#pragma unroll
+  for (int i = 0; i < PER; ++i) {
+    const int seq = PER * lane + i;
+    const SeqSpan sp = seq_span(b, seq < b.seqs ? seq : 0);
+    const bool any = seq < b.seqs && sp.count;
+    tiles[i] = any ? (sp.n + sp.count + 63) / 64 : 0;
+    items[i] = any ? (sp.count * group + cols - 1) / cols : 0;
+    longest = tiles[i] > longest ? tiles[i] : longest;
+    total += items[i] * (tiles[i] + kItemTiles);           // (tiles < 2^25, items <= 2^9 of the workgroup's grid: the host holds their product)
+  }
+#pragma unroll
+  for (int o = 32; o; o >>= 1) {
+    const int other = __shfl_xor(longest, o, 64);
+    longest = other > longest ? other : longest;
+  }
+  total = wave_total(total);
+  if (!total) return false;
+  const int room = (int)gridDim.x / b.Hkv;                 // parts of a head
+  int lo = (total + room - 1) / room, hi = longest + kItemTiles;
+  lo = lo > least ? lo : least;
+  auto parts_of = [&](int tiles_i, int T) { return (tiles_i + kItemTiles + T - 1) / T; };
+  auto parts_at = [&](int T) {
+    int n = 0;
+#pragma unroll
+    for (int i = 0; i < PER; ++i) n += items[i] ? items[i] * parts_of(tiles[i], T) : 0;
+    return n;
+  };
+  while (lo < hi) {                                        // (at hi every item is one part, and the grid holds all items)
+    const int mid = (lo + hi) / 2;
+    if (wave_total(parts_at(mid)) <= room) hi = mid;
+    else lo = mid + 1;
+  }
+  const int T = lo, mine = parts_at(T);
+  int run = mine;
 #pragma unroll
   for (int o = 1; o < 64; o <<= 1) {
-    const int64_t other = __shfl_up((long long)run, o, 64);
+    const int other = __shfl_up(run, o, 64);
     if (lane >= o) run += other;
   }
-  if (lane == 63) sh.part[wave] = run;
-  __syncthreads();
-  int64_t front = 0;
-  for (int w = 0; w < wave; ++w) front += sh.part[w];
-  if (tid < kShareSeqs) sh.before[tid + 1] = front + run;
-  if (tid == 0) sh.before[0] = 0;
-  __syncthreads();
-  return sh.before[b.seqs];
-}
-__device__ __forceinline__ int64_t quota_of(int64_t head_tiles, int Hkv, int workgroups, int least) {
-  const int64_t q = (head_tiles * Hkv + workgroups - 1) / workgroups;
-  return q > least ? q : least;
-}
-// The last sequence that starts at or before tile `at` and has tiles; every lane
-__device__ __forceinline__ int sequence_at(const Share& sh, int seqs, int64_t at, int lane) {
-  int seq = 0;
-  for (int i = 0; i < seqs; i += 64) seq += __popcll(__ballot(i + lane < seqs && sh.before[i + lane + 1] <= at));
-  return seq;
-}
-__device__ __forceinline__ int64_t uniform(int64_t v) {
-  return (int64_t)((uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((int)(v >> 32)) << 32 | (uint32_t)__builtin_amdgcn_readfirstlane((int)v));
-}
-// One item's part in a workgroup's row of tiles
-struct Segment {
-  int seq, hk, col_tile, key0, key1;
-  bool whole;
-  int place;                                 // of the partial result, if not whole
-  int first, parts, first_place;             // the workgroups that share the item: the first one, how many, the first one's place
-};
-// What a workgroup leaves for the join of each of its two places; parts 0: nothing
-struct PartNote {
-  int32_t seq, hk, col_tile, first, parts, first_place, pad[2];
-};
-__device__ __forceinline__ Segment segment_at(const Share& sh, const PagedRows& b, int64_t head_tiles, int64_t u, int64_t end, int64_t begin,
-                                              int64_t quota, int workgroup, int lane) {
-  Segment s;
-  s.hk = (int)(u / head_tiles);
-  const int64_t at = u - s.hk * head_tiles;
-  s.seq = __builtin_amdgcn_readfirstlane(sequence_at(sh, b.seqs, at, lane));
-  const SeqSpan sp = seq_span(b, s.seq);
-  const int tiles = (sp.n + sp.count + 63) / 64;
-  const int64_t in = at - uniform(sh.before[s.seq]);
-  s.col_tile = (int)(in / tiles);
-  const int first = (int)(in - (int64_t)s.col_tile * tiles);
-  const int64_t left = end - u;
-  const int count = left < tiles - first ? (int)left : tiles - first;
-  s.key0 = first * 64;
-  s.key1 = (first + count) * 64 < sp.n + sp.count ? (first + count) * 64 : sp.n + sp.count;
-  s.whole = count == tiles;
-  s.place = workgroup * 2 + (u == begin ? 0 : 1);
-  if (!s.whole) {
-    const int64_t u0 = u - first;
-    s.first = (int)(u0 / quota);
-    s.parts = (int)((u0 + tiles - 1) / quota) - s.first + 1;
-    s.first_place = s.first * quota == u0 ? 0 : 1;
+  const int of_head = __builtin_amdgcn_readlane(run, 63);
+  const int per = gridDim.x / 8, w = gridDim.x % 8 ? blockIdx.x : blockIdx.x % 8 * per + blockIdx.x / 8;
+  if (w >= of_head * b.Hkv) return false;
+  const int hk = w / of_head, at = w - hk * of_head;
+  const int who = __popcll(__ballot(run <= at));           // the lane whose sequences hold part `at`
+  int rest = at - (run - mine), seq = 0, ct = 0, part = 0, parts = 0, n_tiles = 0;
+#pragma unroll
+  for (int i = PER - 1; i >= 0; --i) {                     // from the last: the first that `rest` falls into stays
+    int before = 0;
+#pragma unroll
+    for (int k = 0; k < i; ++k) before += items[k] ? items[k] * parts_of(tiles[k], T) : 0;
+    const int p = items[i] ? parts_of(tiles[i], T) : 1, in = rest - before;
+    if (in >= 0 && in < items[i] * p) seq = PER * lane + i, ct = in / p, part = in - ct * p, parts = p, n_tiles = tiles[i];
   }
-  return s;
+  seq = __builtin_amdgcn_readlane(seq, who), ct = __builtin_amdgcn_readlane(ct, who), part = __builtin_amdgcn_readlane(part, who);
+  parts = __builtin_amdgcn_readlane(parts, who), n_tiles = __builtin_amdgcn_readlane(n_tiles, who);
+  const SeqSpan sp = seq_span(b, seq);
+  int t0, t1;
+  even_share(n_tiles, parts, part, t0, t1);
+  out = Part{seq, hk, ct, t0 * 64, t1 * 64 < sp.n + sp.count ? t1 * 64 : sp.n + sp.count, parts, part, w};
+  return true;
 }
-__device__ __forceinline__ int shared_workgroup() {         // the number of this workgroup in the row
-  const int w = blockIdx.x, per = gridDim.x / 8;
-  return gridDim.x % 8 ? w : w % 8 * per + w / 8;
-}
-
-// The segments of this workgroup, one after the other
-template <int COLS, typename F>
-__device__ __forceinline__ void shared_items(Share& sh, const PagedRows& b, const AttnRows& a, int least, PartNote* notes, F&& item) {
-  const int group = a.Hq / b.Hkv;
-  const bool alone = b.seqs > kShareSeqs;                  // an item to a workgroup
-  int64_t head_tiles = 1, begin = 0, end = 1, quota = 1;
-  const int w = shared_workgroup();
-  bool noted[2] = {false, false};
-  if (!alone) {
-    head_tiles = uniform(share_out(sh, b, group, COLS));
-    quota = quota_of(head_tiles, b.Hkv, gridDim.x, least);
-    const int64_t all = head_tiles * b.Hkv;
-    begin = w * quota;
-    end = begin + quota < all ? begin + quota : all;
-  }
-  for (int64_t u = begin; u < end;) {
-    Segment s;
-    if (alone) {
-      const SeqSpan sp = seq_span(b, blockIdx.z);
-      if ((int)blockIdx.y * COLS >= sp.count * group) return;
-      s = Segment{(int)blockIdx.z, (int)blockIdx.x, (int)blockIdx.y, 0, sp.n + sp.count, true, 0, 0, 0, 0};
-    } else {
-      s = segment_at(sh, b, head_tiles, u, end, begin, quota, w, threadIdx.x & 63);
-      if (!s.whole) {
-        if (threadIdx.x == 0) notes[s.place] = PartNote{s.seq, s.hk, s.col_tile, s.first, s.parts, s.first_place, {0, 0}};
-        noted[s.place & 1] = true;
-      }
-    }
-    int lane = threadIdx.x & 63;
-    asm volatile("" : "+v"(lane));                         // what an item works out from it is not kept from item to item
-    item(s, lane);
-    if (alone) return;
-    u += (s.key1 - s.key0 + 63) / 64;
-    __syncthreads();                                       // (the next one's tiles go where the last one's are read)
-  }
-  if (!alone && threadIdx.x < 2 && !noted[threadIdx.x & 1]) notes[w * 2 + threadIdx.x].parts = 0;
+__device__ __forceinline__ void leave_note(PartNote* notes, int least, bool any, const Part& s) {
+  if (threadIdx.x || !least) return;
+  const int per = gridDim.x / 8, w = gridDim.x % 8 ? blockIdx.x : blockIdx.x % 8 * per + blockIdx.x / 8;
+  notes[w] = any ? PartNote{s.seq, s.hk, s.col_tile, s.part, s.parts, {}} : PartNote{0, 0, 0, 0, 0, {}};
 }
 
 }  // namespace
@@ -731,10 +704,13 @@ __global__ __launch_bounds__(64 * NW, 2) void paged_attn_tile_kernel(PagedRows b
   using Cols = Columns<HD, QB>;
   constexpr int EB = Cols::EB, TILE = 64 * HD * 2, COLS = NW * QB * 16;
   __shared__ __attribute__((aligned(1024))) unsigned char lds[4 * TILE];   // two stages of (K tile, V tile)
-  __shared__ Share sh;
   __shared__ int odd;
-  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), group = a.Hq / b.Hkv;
-  auto item = [&](const Segment& s, int lane) __attribute__((always_inline)) {
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, group = a.Hq / b.Hkv;
+  Part s;
+  const bool any = part_of_workgroup(b, group, COLS, least, s);
+  leave_note(notes, least, any, s);
+  if (!any) return;
+  {
     const int r16 = lane & 15, g = lane >> 4;
     const SeqSpan sp = seq_span(b, s.seq);
     const int col0 = s.col_tile * COLS + wave * QB * 16;
@@ -764,7 +740,7 @@ __global__ __launch_bounds__(64 * NW, 2) void paged_attn_tile_kernel(PagedRows b
 #pragma unroll
     for (int qb = 0; qb < QB; ++qb) {
       const float sum = sum_over_groups(cols.l[qb]);
-      if (s.whole) {
+      if (s.parts == 1) {
 #pragma unroll
         for (int eb = 0; eb < EB; ++eb) cols.finish(a, sp, qb, cols.o[qb][eb], eb, sum, g, nullptr);
       } else {
@@ -774,8 +750,7 @@ __global__ __launch_bounds__(64 * NW, 2) void paged_attn_tile_kernel(PagedRows b
         if (g == 0) *(float2*)(part_ml + at * 2) = make_float2(cols.m[qb], sum);
       }
     }
-  };
-  shared_items<COLS>(sh, b, a, least, notes, item);
+  }
 }
 
 // Many columns: 32 to a wavefront, on the 32 x 32 x 16 instructions (half as many to issue, and a column lies in two lanes instead of
@@ -959,10 +934,13 @@ __global__ __launch_bounds__(256, 2) void paged_attn_wide_kernel(PagedRows b, At
   constexpr int EB = Cols::EB, TILE = 64 * HD * 2, COLS = 128, PIECES = HD / 8, ROWS = 64 / PIECES, PASS = 4 * ROWS, LOADS = 64 / PASS;
   __shared__ __attribute__((aligned(1024))) unsigned char lds[4 * TILE];   // K, K, V, V
   __shared__ uint64_t masks[COLS][kMaskWords];                             // of the item's rows
-  __shared__ Share sh;
-  __shared__ int odd;
-  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), group = a.Hq / b.Hkv;
-  auto item = [&](const Segment& sl, int lane) __attribute__((always_inline)) {
+  __shared__ int odd, missing_from;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, group = a.Hq / b.Hkv;
+  Part sl;
+  const bool any = part_of_workgroup(b, group, COLS, least, sl);
+  leave_note(notes, least, any, sl);
+  if (!any) return;
+  {
     const int half = lane >> 5;
     const SeqSpan sp = seq_span(b, sl.seq);
     const int wg_col0 = sl.col_tile * COLS;
@@ -1002,39 +980,41 @@ __global__ __launch_bounds__(256, 2) void paged_attn_wide_kernel(PagedRows b, At
     Cols cols;
     cols.start(a, sp, sl.hk, group, wg_col0 + wave * 32 + (lane & 31), half);
     const int row0 = wg_col0 / group;
-    if (a.anc && sl.key1 > sp.n) {
-      const int rows = sp.count - row0 < COLS ? sp.count - row0 : COLS;
-      for (int i = wave * 64 + lane; i < rows * kMaskWords; i += 256) masks[i / kMaskWords][i % kMaskWords] = a.anc[(size_t)(sp.row0 + row0) * kMaskWords + i];
+    if (threadIdx.x == 0) odd = 0, missing_from = INT32_MAX;
+    // what is read once: the rows' masks, and whether pages are missing; requested together
+    const int mask_words = !a.anc || sl.key1 <= sp.n ? 0 : (sp.count - row0 < COLS ? sp.count - row0 : COLS) * kMaskWords;
+    uint64_t mask_word[2];
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const int w = threadIdx.x + 256 * i;
+      mask_word[i] = w < mask_words ? a.anc[(size_t)(sp.row0 + row0) * kMaskWords + w] : 0ull;
     }
-    if (threadIdx.x == 0) odd = 0;
-    // tiles in front that every column sees whole, and whether a page is missing
-    int whole = sp.n > sl.key0 ? (sp.n - sl.key0) / 64 : 0;
-    whole = whole < tiles ? whole : tiles;
-    bool missing = false;
-    for (int i = 0; i < tiles; i += 64) {                  // a lane a tile
-      bool bad = false;
-      if (i + lane < tiles)
-        for (int r = 0; r < 64; r += 1 << (in.shift < 6 ? in.shift : 6)) {
-          const int slot = sl.key0 + 64 * (i + lane) + r;
-          bad |= (unsigned)in.table[(slot < in.S ? slot : in.S - 1) >> in.shift] >= (unsigned)in.n_pages;
-        }
-      const uint64_t any = __ballot(bad);
-      if (any) {
-        const int first = i + __builtin_ctzll(any);
-        whole = first < whole ? first : whole;
-        missing = true;
-        break;
-      }
-    }
+    const int page0 = sl.key0 >> in.shift, page1 = (sl.key1 - 1) >> in.shift;
+    int missing = INT32_MAX;
+    for (int i = page0 + threadIdx.x; i <= page1; i += 256)
+      if ((unsigned)in.table[i] >= (unsigned)in.n_pages && i < missing) missing = i;
+    wait_then_barrier();                                   // (odd, missing_from are set)
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+      if ((int)threadIdx.x + 256 * i < mask_words) ((uint64_t*)masks)[threadIdx.x + 256 * i] = mask_word[i];
+    if (missing != INT32_MAX) atomicMin(&missing_from, missing);
     cols.arrived();
     wait_then_barrier();
+    // tiles in front that every column sees whole
+    const int gap = __builtin_amdgcn_readfirstlane(missing_from);
+    int whole = sp.n > sl.key0 ? (sp.n - sl.key0) / 64 : 0;
+    whole = whole < tiles ? whole : tiles;
+    if (gap != INT32_MAX) {
+      const int slot = gap << in.shift, first = slot > sl.key0 ? (slot - sl.key0) / 64 : 0;
+      whole = first < whole ? first : whole;
+    }
     float p[2][16];
     Frag pf[4];
     if (works) cols.template scores<2>(lds, p, lane);
     auto step = [&](auto masked, int t) __attribute__((always_inline)) {
       constexpr bool MASKED = decltype(masked)::value;
       const int j0 = sl.key0 + 64 * t;
-      const uint64_t there = !MASKED ? ~0ull : missing ? in.there_at(j0) : in.up_to_end(j0);
+      const uint64_t there = !MASKED ? ~0ull : gap != INT32_MAX ? in.there_at(j0) : in.up_to_end(j0);
       if (works) {
         uint64_t vis = 0;
         if (MASKED) vis = seen_bits(a.anc ? masks[cols.row < sp.count ? cols.row - row0 : 0] : nullptr, sp, cols.row, j0, there);
@@ -1067,30 +1047,37 @@ __global__ __launch_bounds__(256, 2) void paged_attn_wide_kernel(PagedRows b, At
     for (; t < tiles; ++t) step(std::true_type{}, t);
     if (works && odd) cols.add_odd_values(a, sp, in, sl.key0 + 64 * whole, sl.key1, half);
 
-    if (!works) return;
     auto sw = __builtin_amdgcn_permlane32_swap(__float_as_uint(cols.l), __float_as_uint(cols.l), false, false);
     const float sum = __uint_as_float(sw[0]) + __uint_as_float(sw[1]);
-    if (!sl.whole) {
-      const size_t column = (size_t)sl.place * COLS + wave * 32 + (lane & 31);
-      float* po = part_o + column * HD + half * 4;
+    const bool partial = sl.parts > 1;
+    const float factor = partial ? 1.0f : sum == 0.f ? 0.f : 1.0f / sum;
+    // through LDS, so that a column's row is stored in one piece; 16-byte pieces of a column's HD floats, swizzled by the column
+    __syncthreads();
+    floatx4_t* rows = (floatx4_t*)lds + wave * 32 * (HD / 4);
+    const int r32 = lane & 31;
+    constexpr int QUADS = HD / 4, PER = 64 / QUADS;        // columns an instruction stores
+    if (works) {
 #pragma unroll
-      for (int eb = 0; eb < EB; ++eb)
+      for (int x = 0; x < EB * 4; ++x) {
+        floatx4_t y;
 #pragma unroll
-        for (int a4 = 0; a4 < 4; ++a4)
-          *(float4*)(po + eb * 32 + a4 * 8) = make_float4(cols.o[eb][a4 * 4], cols.o[eb][a4 * 4 + 1], cols.o[eb][a4 * 4 + 2], cols.o[eb][a4 * 4 + 3]);
-      if (half == 0) *(float2*)(part_ml + column * 2) = make_float2(cols.m, sum);
-    } else if (cols.row < sp.count) {
-      const float inv = sum == 0.f ? 0.f : 1.0f / sum;
-      bf16_t* out = (bf16_t*)a.out + (int64_t)(sp.row0 + cols.row) * a.out_stride + (int64_t)cols.head * HD + half * 4;
-#pragma unroll
-      for (int eb = 0; eb < EB; ++eb)
-#pragma unroll
-        for (int a4 = 0; a4 < 4; ++a4)
-          ((Loose8*)(out + eb * 32 + a4 * 8))->v = sum == 0.f ? make_uint2(0, 0) :
-              pack4_bf16(cols.o[eb][a4 * 4] * inv, cols.o[eb][a4 * 4 + 1] * inv, cols.o[eb][a4 * 4 + 2] * inv, cols.o[eb][a4 * 4 + 3] * inv);
+        for (int i = 0; i < 4; ++i) y[i] = sum == 0.f ? 0.f : cols.o[x >> 2][(x & 3) * 4 + i] * factor;
+        rows[r32 * QUADS + ((2 * x + half) ^ (r32 & (QUADS - 1)))] = y;
+      }
+      if (partial && half == 0) *(float2*)(part_ml + ((size_t)sl.place * COLS + wave * 32 + r32) * 2) = make_float2(cols.m, sum);
+#pragma unroll 4
+      for (int i = 0; i < 32 / PER; ++i) {
+        const int c = i * PER + lane / QUADS, quad = lane % QUADS, col = wg_col0 + wave * 32 + c, row = col / group;
+        const floatx4_t y = rows[c * QUADS + (quad ^ (c & (QUADS - 1)))];
+        if (partial) {
+          *(floatx4_t*)(part_o + ((size_t)sl.place * COLS + wave * 32 + c) * HD + quad * 4) = y;
+        } else if (row < sp.count) {
+          bf16_t* out = (bf16_t*)a.out + (int64_t)(sp.row0 + row) * a.out_stride + (int64_t)(sl.hk * group + col % group) * HD + quad * 4;
+          ((Loose8*)out)->v = pack4_bf16(y[0], y[1], y[2], y[3]);
+        }
+      }
     }
-  };
-  shared_items<COLS>(sh, b, a, least, notes, item);
+  }
 }
 
 // out = sum_s 2^(m_s - m) O_s / sum_s 2^(m_s - m) l_s over the slices of a sequence, in a fixed order.  A workgroup per (row, head) and
@@ -1154,24 +1141,23 @@ __global__ __launch_bounds__(PARTS * (HD / 4)) void paged_attn_join_kernel(Paged
       sum == 0.f ? make_uint2(0, 0) : pack4_bf16(acc[0] * inv, acc[1] * inv, acc[2] * inv, acc[3] * inv);
 }
 
-// The same for shared-out work.  A workgroup per place; those that hold a part of an item share the item's elements out among them, four
-// elements to a unit, and where that leaves fewer units than threads, the threads share the parts.
+// The same for shared-out work.  A workgroup per part; those of an item share the item's elements out among them, four elements to a unit, and where that leaves fewer units than threads, the threads share the parts.
 template <int HD, int COLS>
 __global__ __launch_bounds__(256) void paged_attn_share_join_kernel(PagedRows b, AttnRows a, const float* part_o, const float* part_ml,
                                                                    const PartNote* notes) {
   const PartNote n = notes[blockIdx.x];
-  if (!n.parts) return;
+  if (n.parts < 2) return;
   constexpr int T = HD / 4, UNITS = COLS * T;
   const SeqSpan sp = seq_span(b, n.seq);
-  const int tid = threadIdx.x, group = a.Hq / b.Hkv, mine = (int)(blockIdx.x >> 1) - n.first;
+  const int tid = threadIdx.x, group = a.Hq / b.Hkv;
   int lo, hi;
-  even_share(UNITS, n.parts, mine, lo, hi);
+  even_share(UNITS, n.parts, n.part, lo, hi);
   int width = 256, groups = 1;                             // units and shares of the parts at a time
   while (width / 2 >= hi - lo && width > 8) width /= 2, groups *= 2;
   const int share = tid / width;
   __shared__ floatx4_t lds_o[256];
   __shared__ float2 lds_ml[256];
-  auto place = [&](int part) { return (size_t)((n.first + part) * 2 + (part ? 0 : n.first_place)) * COLS; };
+  auto place = [&](int part) { return (size_t)(blockIdx.x - n.part + part) * COLS; };
   for (int u0 = lo; u0 < hi; u0 += width) {
     const int unit = u0 + tid % width, col = unit / T, e = unit % T * 4, c = n.col_tile * COLS + col, row = c / group;
     const bool in = unit < hi && row < sp.count;
@@ -1229,7 +1215,7 @@ struct AttnPlan {
   bool simple, few;
   int blocks;                    // few: column blocks of 16
   int split_len, splits;         // few
-  int cols, workgroups, least;   // shared-out work: columns of an item, workgroups (0: one to an item), tiles that are worth one
+  int cols, workgroups, least;   // shared-out work: columns of an item, workgroups (0: one to an item), the least tiles of one
 };
 AttnPlan attn_plan(int dtype, const PagedRows& b, int Hq) {
   AttnPlan p{};
@@ -1250,16 +1236,21 @@ AttnPlan attn_plan(int dtype, const PagedRows& b, int Hq) {
     return p;
   }
   p.cols = cols <= 64 ? 64 : 128;
-  p.least = 4;
-  const int64_t most = (int64_t)b.seqs * b.Hkv * ((cols + p.cols - 1) / p.cols) * ((S + 63) / 64);        // tiles
-  p.workgroups = b.seqs > kShareSeqs ? 0 : 512;
-  if (p.workgroups > (most + p.least - 1) / p.least) p.workgroups = (int)((most + p.least - 1) / p.least);
+  // two workgroups to a compute unit; a grid that holds every item, or an item to a workgroup where there are many
+  const int64_t items = (int64_t)b.seqs * b.Hkv * ((cols + p.cols - 1) / p.cols), tiles = (S + 63) / 64;
+  if (b.seqs <= kShareSeqs && items <= 1024 && items * (tiles + kItemTiles) < 1 << 30) {
+    p.least = 8;
+    p.workgroups = items <= 512 ? 512 : 1024;
+    p.workgroups -= p.workgroups % b.Hkv;                  // (every head has room for its items: Hkv <= items)
+    const int64_t most = items * ((tiles + kItemTiles + p.least - 1) / p.least);       // parts
+    if (p.workgroups > most) p.workgroups = (int)most;
+  }
   return p;
 }
 size_t part_columns(const AttnPlan& p, const PagedRows& b, int Hq) {        // columns of partial results
   if (p.simple) return 0;
   if (p.few) return p.splits > 1 ? (size_t)p.splits * b.rows * Hq : 0;
-  return (size_t)p.workgroups * 2 * p.cols;
+  return (size_t)p.workgroups * p.cols;
 }
 template <int HD>
 hipError_t launch_attn_hd(const AttnPlan& p, const PagedRows& b, const AttnRows& a, float* part_o, float* part_ml, PartNote* notes, hipStream_t s) {
@@ -1279,7 +1270,7 @@ hipError_t launch_attn_hd(const AttnPlan& p, const PagedRows& b, const AttnRows&
   hipLaunchKernelGGL(f, grid, dim3(256), 0, s, b, a, p.least, part_o, part_ml, notes);
   if (p.workgroups > 1) {
     auto j = p.cols == 64 ? paged_attn_share_join_kernel<HD, 64> : paged_attn_share_join_kernel<HD, 128>;
-    hipLaunchKernelGGL(j, dim3(p.workgroups * 2), dim3(256), 0, s, b, a, part_o, part_ml, notes);
+    hipLaunchKernelGGL(j, dim3(p.workgroups), dim3(256), 0, s, b, a, part_o, part_ml, notes);
   }
   return hipGetLastError();
 }
@@ -1287,7 +1278,7 @@ hipError_t launch_attn_hd(const AttnPlan& p, const PagedRows& b, const AttnRows&
 
 size_t paged_attn_scratch_bytes(int dtype, const PagedRows& b, int Hq) {
   const AttnPlan p = attn_plan(dtype, b, Hq);
-  return part_columns(p, b, Hq) * (b.hd + 2) * sizeof(float) + (size_t)p.workgroups * 2 * sizeof(PartNote);
+  return part_columns(p, b, Hq) * (b.hd + 2) * sizeof(float) + (size_t)p.workgroups * sizeof(PartNote);
 }
 
 hipError_t launch_paged_attn(int dtype, const PagedRows& b, const AttnRows& a, void* scratch, hipStream_t s) {
