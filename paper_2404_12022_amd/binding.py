@@ -243,30 +243,35 @@ def _bad(message: str) -> HTError:
     return HTError(HT_EINVAL, message)
 
 
-def _need(t, name, dtype, shape, device, rows_only=False):
-    """The tensor's address, if it is what the call reads: type, shape, device, and contiguous (rows_only: within a row).  None
-    stays None."""
+def _need(t, name, dtype, shape, device):
+    """The tensor's address, if it is what the call reads: type, shape, device, contiguous.  None stays None.  (These checks are a call's
+    price on the host, some 0.5 us each: integers and tuples are compared, no objects made.)"""
     if t is None:
         return None
-    if t.dtype != dtype or tuple(t.shape) != tuple(shape) or t.device != device:
-        raise _bad(f"{name} is {t.dtype} {tuple(t.shape)} on {t.device}, wanted {dtype} {tuple(shape)} on {device}")
-    if rows_only:
-        if t.shape[0] and not t[0].is_contiguous():
-            raise _bad(f"{name} is not contiguous within a row")
-    elif not t.is_contiguous():
-        raise _bad(f"{name} is not contiguous")
-    return t.data_ptr()
+    if t.dtype is dtype and t.shape == shape and t.get_device() == device.index and t.is_contiguous():
+        return t.data_ptr()
+    raise _bad(f"{name} is {t.dtype} {tuple(t.shape)} on {t.device}{'' if t.is_contiguous() else ', not contiguous'}, "
+               f"wanted {dtype} {tuple(shape)} on {device}")
 
 
 def _run(device, stream, fn, *args) -> None:
     """The call on `stream`, or on the current stream of the tensors' device, with that device current."""
     if stream is not None and stream.device != device:
         raise _bad(f"the stream is on {stream.device}, the tensors on {device}")
-    if torch.cuda.current_device() == device.index:
-        _check(fn(*args, _stream_ptr(stream)))
+    if _current_device() == device.index:
+        rc = fn(*args, _stream_ptr(stream))
+        if rc:
+            _check(rc)
     else:
         with torch.cuda.device(device):
             _check(fn(*args, _stream_ptr(stream)))
+
+
+def _current_device() -> int:
+    try:
+        return torch._C._cuda_getDevice()
+    except AttributeError:
+        return torch.cuda.current_device()
 
 
 def _empty(shape, dtype, device, stream):
@@ -313,10 +318,13 @@ class PagedBatch:
         """(address, elements from a row to the next) of [rows, heads, head_dim]."""
         if t is None:
             return None, 0
-        if t.dim() != 3:
-            raise _bad(f"{name} is not [rows, heads, head_dim]")
-        at = _need(t, name, self.dtype, (self.rows, t.shape[1], self.pool[3]), self.device, rows_only=True)
-        return at, t.stride(0) if self.rows > 1 else t.shape[1] * t.shape[2]
+        s, hd = t.shape, self.pool[3]
+        if len(s) == 3 and s[0] == self.rows and s[2] == hd and t.dtype is self.dtype and t.get_device() == self.device.index:
+            step = t.stride()
+            if step[2] == 1 and (step[1] == hd or s[1] == 1):
+                return t.data_ptr(), step[0] if s[0] > 1 else s[1] * hd
+            raise _bad(f"{name} is not contiguous within a row")
+        raise _bad(f"{name} is {t.dtype} {tuple(s)} on {t.device}, wanted {self.dtype} [{self.rows}, heads, {hd}] on {self.device}")
 
 
 def ht_tree_tables(batch: PagedBatch, parent, stream=None):
