@@ -9,13 +9,14 @@
 // of an unfiltered vocabulary falls on the other side of a border.
 //
 // A workgroup of 1024 threads per row, which goes over it a few times; all but the first come from L2.  (Held in registers, with every
-// pass unrolled over them, the passes' own needs went to scratch memory.)  A prefix of the order ends at one element (value, index), so a filter is a search for that element, not a sort of the row.  The r-th largest of
-// the 1024 threads' maxima is no larger than the r-th largest value, so the elements from there on hold the first r; they are a few
-// more than r as a rule, are listed and sorted, and all filters work on the list.  Where the list does not reach (a large k, a flat row),
-// a histogram of counts (top-k) or masses (top-p) over 2048 equal steps of the value finds the step that holds the end, whose
-// elements are listed and ranked; a step that holds too many becomes the next histogram's range (a value far below the others, as masks
-// leave, costs such a round).  Masses of a histogram are counted in whole 2^-43: sums of integers do not depend on the order of the
-// atomics.
+// pass unrolled over them, the passes' own needs went to scratch memory.)  A prefix of the order ends at one element (value, index),
+// so a filter is a search for that element, not a sort of the row:
+//   top-k    the k-th largest of the 1024 threads' maxima is no larger than the k-th largest value, so the elements from there on hold
+//            the first k; they are a few more than k, are listed and sorted, and top-p, min-p and the draw work on the list.
+//   top-p alone, or a k that makes the list too long: a histogram of masses (or counts) over 2048 equal steps of the value finds the
+//            step that holds the end, whose elements are listed and ranked; a step that holds too many becomes the next
+//            histogram's range (a value far below the others, as masks leave, costs such a round).  Its masses are counted in whole
+//            2^-43: sums of integers do not depend on the order of the atomics.
 #include "ht_common.h"
 
 namespace ht {
@@ -23,7 +24,7 @@ namespace ht {
 namespace {
 
 constexpr int kThreads = 1024, kWaves = kThreads / 64, kBins = 2048, kList = 1024;
-constexpr int kMaxima = 512;                 // maxima whose list a top-p without top-k tries first
+constexpr int kShort = 256;                  // list lengths whose order is counted out, not sorted: a sort's steps wait for each other
 
 template <typename T> struct Vec16;
 template <> struct Vec16<float> {
@@ -36,8 +37,6 @@ template <> struct Vec16<bf16_t> {
 template <typename T> struct __attribute__((packed, aligned(sizeof(T)))) Loose16 {
   T v[Vec16<T>::N];
 };
-__device__ inline float widen(float v) { return v; }
-__device__ inline float widen(bf16_t v) { return bf16_to_float(v); }
 // value c of a piece held in four registers
 template <typename T> __device__ inline float value_of(const uint32_t (&w)[4], int c);
 template <> __device__ inline float value_of<float>(const uint32_t (&w)[4], int c) { return __uint_as_float(w[c]); }
@@ -59,26 +58,52 @@ __device__ inline uint32_t ordered(float v) {
 }
 __device__ inline float of_ordered(uint32_t k) { return __uint_as_float(k & 0x80000000u ? k & 0x7fffffffu : ~k); }
 
-// exp of y <= 0: y = n ln 2 + f, |f| <= ln 2 / 2, and the series to f^13 (the first term left out is 4e-18 of the result)
-__device__ inline double exp_below(double y) {
-  constexpr double ln2 = 0.69314718055994531, ln2_rest = 2.3190468138462996e-17, per_ln2 = 1.4426950408889634;
-  y = fmax(y, -800.0);                                     // 0 from -746 on
-  const double n = rint(y * per_ln2), f = fma(n, -ln2_rest, fma(n, -ln2, y));
-  constexpr double c[13] = {1.0, 1.0, 1.0 / 2, 1.0 / 6, 1.0 / 24, 1.0 / 120, 1.0 / 720, 1.0 / 5040, 1.0 / 40320, 1.0 / 362880,
-                            1.0 / 3628800, 1.0 / 39916800, 1.0 / 479001600};
-  double e = 1.0 / 6227020800.0;
+// exp of -1 <= y <= 0, for the table: the series to y^19 (the first term left out is 4e-19)
+__device__ inline double exp_series(double y) {
+  double e = 1.0;
 #pragma unroll
-  for (int i = 12; i >= 0; --i) e = fma(e, f, c[i]);
-  return ldexp(e, (int)n);
+  for (int i = 19; i >= 1; --i) e = fma(e, y * (1.0 / i), 1.0);
+  return e;
 }
 
-template <typename V> __device__ inline V wave_fold(V v, V (*f)(V, V)) {
-  for (int o = 32; o; o >>= 1) v = f(v, __shfl_xor(v, o, 64));
+// Sums and extremes over a wavefront by DPP moves: lane 63 ends with all (a lane that has no partner takes `none`)
+template <int CTRL, int ROWS, typename V> __device__ inline V moved(V v, V none) {
+  if constexpr (sizeof(V) == 4) {
+    const int r = __builtin_amdgcn_update_dpp(__builtin_bit_cast(int, none), __builtin_bit_cast(int, v), CTRL, ROWS, 0xf, false);
+    return __builtin_bit_cast(V, r);
+  } else {
+    const uint64_t n = __builtin_bit_cast(uint64_t, none), u = __builtin_bit_cast(uint64_t, v);
+    const uint32_t lo = __builtin_amdgcn_update_dpp((int)n, (int)u, CTRL, ROWS, 0xf, false);
+    const uint32_t hi = __builtin_amdgcn_update_dpp((int)(n >> 32), (int)(u >> 32), CTRL, ROWS, 0xf, false);
+    return __builtin_bit_cast(V, (uint64_t)hi << 32 | lo);
+  }
+}
+template <typename V> __device__ inline V lane_of(V v, int lane) {
+  if constexpr (sizeof(V) == 4) {
+    return __builtin_bit_cast(V, __builtin_amdgcn_readlane(__builtin_bit_cast(int, v), lane));
+  } else {
+    const uint64_t u = __builtin_bit_cast(uint64_t, v);
+    return __builtin_bit_cast(V, (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(u >> 32), lane) << 32 | (uint32_t)__builtin_amdgcn_readlane((int)u, lane));
+  }
+}
+// Running over the lanes: lane l ends with f of lanes 0 .. l
+template <typename V, typename F> __device__ inline V wave_run(V v, V none, F f) {
+  v = f(moved<0x111, 0xf>(v, none), v);      // row_shr 1, 2, 4, 8; the rows' ends to the rows behind
+  v = f(moved<0x112, 0xf>(v, none), v);
+  v = f(moved<0x114, 0xf>(v, none), v);
+  v = f(moved<0x118, 0xf>(v, none), v);
+  v = f(moved<0x142, 0xa>(v, none), v);
+  v = f(moved<0x143, 0xc>(v, none), v);
   return v;
 }
-template <typename V> __device__ inline V take_sum(V a, V b) { return a + b; }
-template <typename V> __device__ inline V take_max(V a, V b) { return a > b ? a : b; }
-template <typename V> __device__ inline V take_min(V a, V b) { return a < b ? a : b; }
+// ... over 16 values that repeat in every row of 16 lanes: lane 15 ends with all
+template <typename V, typename F> __device__ inline V row_run(V v, V none, F f) {
+  v = f(moved<0x111, 0xf>(v, none), v);
+  v = f(moved<0x112, 0xf>(v, none), v);
+  v = f(moved<0x114, 0xf>(v, none), v);
+  v = f(moved<0x118, 0xf>(v, none), v);
+  return v;
+}
 
 }  // namespace
 
@@ -92,9 +117,13 @@ __global__ __launch_bounds__(kThreads) void sample_rows_kernel(SampleRows a) {
   float* list_x = (float*)(shared_mem + 24576);                                  // [kList]
   int32_t* list_i = (int32_t*)(shared_mem + 28672);                              // [kList]
   double* segs = (double*)shared_mem;                                            // [4096]
+  unsigned long long* loose = (unsigned long long*)(shared_mem + 16384);         // [kList] the list before it is sorted
+  uint32_t* by_index = (uint32_t*)(shared_mem + 8192);                           // [kShort] the kept ones in the order of their indices
+  double* by_index_e = (double*)shared_mem;
   __shared__ unsigned long long keys[kList];                                     // the sorted list: order, then index
   __shared__ double shares[kList];                                               // ... and its e
-  __shared__ unsigned long long fold[kWaves];
+  __shared__ double roots[32];                                                   // 2^(j / 32)
+  __shared__ unsigned long long fold[2][kWaves];
   __shared__ Found found;
 
   const int row = blockIdx.x, tid = threadIdx.x, wave = tid >> 6, lane = tid & 63, V = a.V;
@@ -140,30 +169,43 @@ __global__ __launch_bounds__(kThreads) void sample_rows_kernel(SampleRows a) {
         }
     }
   };
-  auto block_fold = [&](auto v, auto f) __attribute__((always_inline)) {
+  // over the workgroup, one barrier (the slots take turns, so the last fold's may still be read)
+  int turn = 0;
+  auto block_fold = [&](auto v, auto none, auto f) __attribute__((always_inline)) {
     using W = decltype(v);
-    static_assert(sizeof(W) <= 8, "a word per wavefront");
-    v = wave_fold<W>(v, f);
+    W* slots = (W*)fold[turn];
+    turn ^= 1;
+    v = wave_run<W>(v, none, f);
+    if (lane == 63) slots[wave] = v;
     __syncthreads();
-    W* slots = (W*)fold;
-    if (lane == 0) slots[wave] = v;
-    __syncthreads();
-    v = slots[lane & (kWaves - 1)];
-    return wave_fold<W>(v, f);
+    return lane_of(row_run<W>(slots[lane & (kWaves - 1)], none, f), 15);
   };
-  // (a sum over all 64 lanes counts every wavefront's word four times)
-  auto block_sum = [&](unsigned long long v) __attribute__((always_inline)) { return block_fold(v, take_sum<unsigned long long>) / (64 / kWaves); };
+  auto add = [](auto x, auto y) __attribute__((always_inline)) { return x + y; };
+  auto larger = [](auto x, auto y) __attribute__((always_inline)) { return x > y ? x : y; };
+  auto smaller = [](auto x, auto y) __attribute__((always_inline)) { return x < y ? x : y; };
+  auto count = [&](int n) __attribute__((always_inline)) -> int { return block_fold(n, 0, add); };
+  // sums up to every thread
+  auto block_run = [&](auto v, auto none) __attribute__((always_inline)) {
+    using W = decltype(v);
+    W* slots = (W*)fold[turn];
+    turn ^= 1;
+    v = wave_run<W>(v, none, add);
+    if (lane == 63) slots[wave] = v;
+    __syncthreads();
+    const W ends = row_run<W>(slots[lane & (kWaves - 1)], none, add);
+    return wave ? v + lane_of(ends, wave - 1) : v;
+  };
 
-  float top = -INFINITY, low = INFINITY;
+  if (tid < 32) roots[tid] = tid ? 2.0 * exp_series((tid - 32) * (0.69314718055994531 / 32.0)) : 1.0;
+  float best = -INFINITY, low = INFINITY;                  // this thread's largest value, the smallest one
   each([&](int, const float(&x)[VEC], int) __attribute__((always_inline)) {
 #pragma unroll
     for (int c = 0; c < VEC; ++c) {
-      top = fmaxf(top, x[c]);
+      best = fmaxf(best, x[c]);
       if (x[c] > -INFINITY) low = fminf(low, x[c]);
     }
   });
-  const float my_top = top;
-  top = block_fold(top, take_max<float>);
+  float top = block_fold(best, -INFINITY, larger);
   if (top == -INFINITY) {                                  // nothing to draw from
     if (tid == 0) {
       a.tokens[row] = -1;
@@ -174,12 +216,13 @@ __global__ __launch_bounds__(kThreads) void sample_rows_kernel(SampleRows a) {
   const float temp = a.temperature ? a.temperature[row] : 1.0f;
   if (!(temp > 0.f)) {
     int first = INT32_MAX;
-    each([&](int, const float(&x)[VEC], int i0) __attribute__((always_inline)) {
+    if (best == top)
+      each([&](int, const float(&x)[VEC], int i0) __attribute__((always_inline)) {
 #pragma unroll
-      for (int c = VEC - 1; c >= 0; --c)
-        if (x[c] == top && i0 + c < first) first = i0 + c;
-    });
-    first = block_fold(first, take_min<int>);
+        for (int c = VEC - 1; c >= 0; --c)
+          if (x[c] == top && i0 + c < first) first = i0 + c;
+      });
+    first = block_fold(first, INT32_MAX, smaller);
     if (tid == 0) {
       a.tokens[row] = first;
       if (a.logprob) a.logprob[row] = 0.f;
@@ -188,40 +231,56 @@ __global__ __launch_bounds__(kThreads) void sample_rows_kernel(SampleRows a) {
   }
   if (top == INFINITY) {
     spike = true;
+    best = best == INFINITY ? 0.f : -INFINITY;
     top = low = 0.f;
-  } else {
-    low = block_fold(low, take_min<float>);
   }
-  const double per_temp = 1.0 / (double)temp;
+  // e = 2^(y / 32), y = 32 (x - top) / (T ln 2) = n + f, |f| <= 1/2: a table for n modulo 32, a power of two, and the series of 2^(f / 32) to
+  // f^5 (the first term left out is 2e-15).  y is 0 at the maximum and e is 1.  12 operations in 64 bits; with the series of the whole
+  // exponential (20) the pass over 32000 values of one row took 16 us
+  const double steepness = 46.166241308446828 / (double)temp;          // 32 / ln 2
   auto energy = [&](float x) __attribute__((always_inline)) -> double {
-    return x == top ? 1.0 : x == -INFINITY ? 0.0 : exp_below(((double)x - (double)top) * per_temp);
+    constexpr double s = 0.69314718055994531 / 32.0, c1 = s, c2 = s * s / 2, c3 = s * s * s / 6, c4 = s * s * s * s / 24, c5 = s * s * s * s * s / 120;
+    const double y = fmax(((double)x - (double)top) * steepness, -60000.0);      // (-inf, and its product with 0: e is 0)
+    const double n = rint(y), f = y - n;
+    const int k = (int)n;
+    const double p = f * fma(f, fma(f, fma(f, fma(f, c5, c4), c3), c2), c1), root = roots[k & 31];
+    return ldexp(fma(root, p, root), k >> 5);
   };
   // in whole 2^-43, up to 2^20 of them in 64 bits: the mantissa's end of e + 512
   auto whole = [&](float x) __attribute__((always_inline)) -> unsigned long long {
     return (unsigned long long)__double_as_longlong(energy(x) + 512.0) - 0x4080000000000000ull;
   };
 
-  const float best = !spike ? my_top : my_top == INFINITY ? 0.f : -INFINITY;       // this thread's largest value
   float cut_x = -INFINITY;                                 // kept so far: what comes before or is (cut_x, cut_i)
   int cut_i = -1;
   auto kept = [&](float x, int i) __attribute__((always_inline)) { return x > cut_x || (x == cut_x && i <= cut_i); };
 
-  // the element of the kept ones at which the running weight reaches `need` (at least 1) becomes the cut; none if it never does
-  auto search = [&](auto weight, unsigned long long need, float floor_x) __attribute__((always_inline)) {
-    float lo = fmaxf(fmaxf(cut_x, low), floor_x), hi = top;
+  // the element of the kept ones at which the running weight reaches `need` (at least 1), or a share of all the weight from lo on where
+  // `share` is not negative, becomes the cut; none if it never does.  Elements above hi or below lo are left alone
+  auto search = [&](auto weight, unsigned long long need, double share, float lo, float hi) __attribute__((always_inline)) {
     unsigned long long above = 0;
     for (;;) {
       if (lo == hi) {                                      // equal values: the lowest indices, as many as it takes
-        const unsigned long long w = weight(hi), r = w ? (need - above + w - 1) / w : 1;
+        const unsigned long long w = weight(hi);
+        if (share >= 0.0) {
+          int all = 0;
+          each([&](int, const float(&x)[VEC], int i0) __attribute__((always_inline)) {
+#pragma unroll
+            for (int c = 0; c < VEC; ++c) all += x[c] == hi && kept(x[c], i0 + c);
+          });
+          need = (unsigned long long)ceil(share * (double)((unsigned long long)count(all) * w));
+          need = need ? need : 1;
+        }
+        const unsigned long long r = w ? (need - above + w - 1) / w : 1;
         int at = 0, end = V;                               // smallest index with r of them up to it
         while (at < end) {
           const int mid = (at + end) / 2;
-          unsigned long long n = 0;
+          int n = 0;
           each([&](int, const float(&x)[VEC], int i0) __attribute__((always_inline)) {
 #pragma unroll
             for (int c = 0; c < VEC; ++c) n += x[c] == hi && kept(x[c], i0 + c) && i0 + c <= mid;
           });
-          if (block_sum(n) >= r) end = mid;
+          if ((unsigned long long)count(n) >= r) end = mid;
           else at = mid + 1;
         }
         if (at < V) cut_x = hi, cut_i = at;
@@ -239,23 +298,25 @@ __global__ __launch_bounds__(kThreads) void sample_rows_kernel(SampleRows a) {
       each([&](int, const float(&x)[VEC], int i0) __attribute__((always_inline)) {
 #pragma unroll
         for (int c = 0; c < VEC; ++c)
-          if (x[c] >= lo && x[c] <= hi && kept(x[c], i0 + c)) atomicAdd(&hist[bin_of(x[c])], weight(x[c]));
+          if (x[c] >= lo && x[c] <= hi && kept(x[c], i0 + c)) {
+            const unsigned long long w = weight(x[c]);
+            if (w) atomicAdd(&hist[bin_of(x[c])], w);
+          }
       });
       __syncthreads();
-      {                                                    // two steps a thread
-        const unsigned long long h0 = hist[2 * tid], h1 = hist[2 * tid + 1];
-        unsigned long long run = h0 + h1;
-        for (int o = 1; o < 64; o <<= 1) {
-          const unsigned long long other = __shfl_up(run, o, 64);
-          if (lane >= o) run += other;
-        }
-        if (lane == 63) fold[wave] = run;
+      const unsigned long long h0 = hist[2 * tid], h1 = hist[2 * tid + 1];       // two steps a thread
+      const unsigned long long run = block_run(h0 + h1, 0ull);
+      if (share >= 0.0) {
+        if (tid == kThreads - 1) found.above = run;
         __syncthreads();
-        unsigned long long before = above + run - h0 - h1;
-        for (int w = 0; w < wave; ++w) before += fold[w];
-        if (before < need && before + h0 >= need) found.bin = 2 * tid, found.above = before;
-        else if (before + h0 < need && before + h0 + h1 >= need) found.bin = 2 * tid + 1, found.above = before + h0;
+        need = (unsigned long long)ceil(share * (double)found.above);
+        need = need ? need : 1;
+        share = -1.0;
+        __syncthreads();
       }
+      const unsigned long long before = above + run - h0 - h1;
+      if (before < need && before + h0 >= need) found.bin = 2 * tid, found.above = before;
+      else if (before + h0 < need && before + h0 + h1 >= need) found.bin = 2 * tid + 1, found.above = before + h0;
       __syncthreads();
       const int bin = found.bin;
       if (bin < 0) return;
@@ -263,7 +324,7 @@ __global__ __launch_bounds__(kThreads) void sample_rows_kernel(SampleRows a) {
       each([&](int, const float(&x)[VEC], int i0) __attribute__((always_inline)) {
 #pragma unroll
         for (int c = 0; c < VEC; ++c)
-          if (x[c] >= lo && x[c] <= hi && kept(x[c], i0 + c) && bin_of(x[c]) == bin) {
+          if (x[c] >= lo && x[c] <= hi && bin_of(x[c]) == bin && kept(x[c], i0 + c)) {
             const int at = atomicAdd(&found.listed, 1);
             if (at < kList) {
               list_x[at] = x[c];
@@ -283,9 +344,9 @@ __global__ __launch_bounds__(kThreads) void sample_rows_kernel(SampleRows a) {
       if (tid < n) {
         const float x = list_x[tid];
         const int i = list_i[tid];
-        unsigned long long before = above;
-        for (int o = 0; o < n; ++o) before += list_x[o] > x || (list_x[o] == x && list_i[o] < i) ? list_w[o] : 0;
-        if (before < need && before + list_w[tid] >= need) found.value = x, found.index = i;
+        unsigned long long front = above;
+        for (int o = 0; o < n; ++o) front += list_x[o] > x || (list_x[o] == x && list_i[o] < i) ? list_w[o] : 0;
+        if (front < need && front + list_w[tid] >= need) found.value = x, found.index = i;
       }
       __syncthreads();
       cut_x = found.value, cut_i = found.index;
@@ -293,95 +354,86 @@ __global__ __launch_bounds__(kThreads) void sample_rows_kernel(SampleRows a) {
     }
   };
 
-  // A value that no more than its own thread's larger ones can be ... : at least `r` elements are no smaller (-inf: all)
+  // A value that at least r elements are no smaller than: the r-th largest of the threads' maxima, or a little below (-inf where there
+  // are not so many maxima)
   auto floor_of = [&](int r) __attribute__((always_inline)) -> float {
     uint32_t* bins = (uint32_t*)shared_mem;                // 1024 steps
-    __syncthreads();
     bins[tid] = 0;
     if (tid == 0) found.bin = -1;
-    const float least_best = block_fold(best > -INFINITY ? best : top, take_min<float>);   // (barriers)
-    const float steps = 1024.0f / (top - least_best);
+    const float worst = block_fold(best > -INFINITY ? best : top, top, smaller);           // (a barrier)
+    const float steps = 1024.0f / (top - worst);
     auto bin_of = [&](float x) __attribute__((always_inline)) {
       const float n = (top - x) * steps;
       return n < 1023.0f ? (int)n : n >= 1023.0f ? 1023 : 0;          // (equal values, or a range past the largest float: 0)
     };
     if (best > -INFINITY) atomicAdd(&bins[bin_of(best)], 1u);
     __syncthreads();
-    uint32_t run = bins[tid];
-    for (int o = 1; o < 64; o <<= 1) {
-      const uint32_t other = __shfl_up(run, o, 64);
-      if (lane >= o) run += other;
-    }
-    if (lane == 63) fold[wave] = run;
-    __syncthreads();
-    uint32_t before = run - bins[tid];
-    for (int w = 0; w < wave; ++w) before += (uint32_t)fold[w];
-    if (before < (uint32_t)r && before + bins[tid] >= (uint32_t)r) found.bin = tid;
+    const int mine = (int)bins[tid], before = block_run(mine, 0) - mine;
+    if (before < r && before + mine >= r) found.bin = tid;
     __syncthreads();
     const int bin = found.bin;
     // the smallest of the maxima in that step and above
-    float v = bin >= 0 && best > -INFINITY && bin_of(best) <= bin ? best : top;
-    v = block_fold(v, take_min<float>);
+    const float v = block_fold(bin >= 0 && best > -INFINITY && bin_of(best) <= bin ? best : top, top, smaller);
     return bin < 0 ? -INFINITY : v;
   };
   // The elements from `from` on, sorted: their number, or more than kList if they are too many to list
   auto list_from = [&](float from) __attribute__((always_inline)) -> int {
-    __syncthreads();
     if (tid == 0) found.listed = 0;
     __syncthreads();
-    each([&](int, const float(&x)[VEC], int i0) __attribute__((always_inline)) {
+    if (best >= from)
+      each([&](int, const float(&x)[VEC], int i0) __attribute__((always_inline)) {
+        bool some = false;
 #pragma unroll
-      for (int c = 0; c < VEC; ++c)
-        if (x[c] >= from && x[c] > -INFINITY) {
-          const int at = atomicAdd(&found.listed, 1);
-          if (at < kList) keys[at] = (unsigned long long)~ordered(x[c]) << 32 | (uint32_t)(i0 + c);
-        }
-    });
+        for (int c = 0; c < VEC; ++c) some |= x[c] >= from;
+        if (!some) return;
+#pragma unroll
+        for (int c = 0; c < VEC; ++c)
+          if (x[c] >= from && x[c] > -INFINITY) {
+            const int at = atomicAdd(&found.listed, 1);
+            if (at < kList) loose[at] = (unsigned long long)~ordered(x[c]) << 32 | (uint32_t)(i0 + c);
+          }
+      });
     __syncthreads();
     const int n = found.listed;
     if (n > kList) return n;
-    int size = 64;
-    while (size < n) size *= 2;
-    unsigned long long key = tid < n ? keys[tid] : ~0ull;
-    // bitonic: strides below 64 inside a wavefront
-    for (int half = 2; half <= size; half *= 2)
-      for (int stride = half / 2; stride; stride /= 2) {
-        unsigned long long other;
-        if (stride >= 64) {
-          __syncthreads();
-          if (tid < size) keys[tid] = key;
-          __syncthreads();
-          other = tid < size ? keys[tid ^ stride] : 0;
-        } else {
-          if (wave * 64 >= size) continue;
-          other = __shfl_xor(key, stride, 64);
-        }
-        const bool up = (tid & half) == 0, first = (tid & stride) == 0;
-        key = (other < key) == (up == first) ? other : key;
+    if (n <= kShort) {
+      // four threads count a quarter of the list each for an element
+      const int who = tid >> 2, part = tid & 3;
+      const unsigned long long key = who < n ? loose[who] : 0;
+      int rank = 0;
+      for (int o = part; o < n; o += 4) rank += loose[o] < key;
+      rank += __shfl_xor(rank, 1, 64);
+      rank += __shfl_xor(rank, 2, 64);
+      if (who < n && part == 0) {
+        keys[rank] = key;
+        shares[rank] = energy(of_ordered(~(uint32_t)(key >> 32)));
       }
-    __syncthreads();
-    if (tid < size) keys[tid] = key;
-    if (tid < n) shares[tid] = energy(of_ordered(~(uint32_t)(key >> 32)));
-    __syncthreads();
-    return n;
-  };
-  // Sum of the list's e up to element `tid` (zeros behind the list)
-  auto list_sums = [&](int n) __attribute__((always_inline)) -> double {
-    double run = tid < n ? shares[tid] : 0.0;
-    for (int o = 1; o < 64; o <<= 1) {
-      const double other = __shfl_up(run, o, 64);
-      if (lane >= o) run += other;
+    } else {
+      // bitonic, strides below 64 inside a wavefront
+      int size = 512;
+      while (size < n) size *= 2;
+      unsigned long long key = tid < n ? loose[tid] : ~0ull;
+      for (int half = 2; half <= size; half *= 2)
+        for (int stride = half / 2; stride; stride /= 2) {
+          unsigned long long other;
+          if (stride >= 64) {
+            __syncthreads();
+            if (tid < size) keys[tid] = key;
+            __syncthreads();
+            other = tid < size ? keys[tid ^ stride] : 0;
+          } else {
+            if (wave * 64 >= size) continue;
+            other = __shfl_xor(key, stride, 64);
+          }
+          const bool up = (tid & half) == 0, first = (tid & stride) == 0;
+          key = (other < key) == (up == first) ? other : key;
+        }
+      __syncthreads();
+      if (tid < size) keys[tid] = key;
+      if (tid < n) shares[tid] = energy(of_ordered(~(uint32_t)(key >> 32)));
     }
     __syncthreads();
-    double* ends = (double*)fold;
-    if (lane == 63) ends[wave] = run;
-    __syncthreads();
-    double before = 0.0;
-    for (int w = 0; w < wave; ++w) before += ends[w];
-    return before + run;
-  };
-  auto cut_at = [&](int i) __attribute__((always_inline)) {          // element i of the list ends what is kept
-    cut_x = of_ordered(~(uint32_t)(keys[i] >> 32)), cut_i = (int)(uint32_t)keys[i];
+    return n;
   };
 
   const int k_in = a.top_k ? a.top_k[row] : 0, k = k_in > 0 && k_in < V ? k_in : 0;
@@ -390,88 +442,64 @@ __global__ __launch_bounds__(kThreads) void sample_rows_kernel(SampleRows a) {
   const double p = p_in > 0.f ? (double)p_in : 0.0;
   const float mp = a.min_p ? a.min_p[row] : 0.f;
   const double least = mp > 0.f ? (mp < 1.f ? (double)mp : 1.0) : 0.0;
-  int listed = 0, kept_list = 0;                           // of the list: elements, and how many of them are kept; 0: no list
-  if (k) {
-    const float from = k <= kThreads ? floor_of(k) : -INFINITY;
-    const int n = k <= kList ? list_from(from) : kList + 1;
-    if (n <= kList) {
-      listed = n;
-      kept_list = k < n ? k : n;
-    } else {
-      search([](float) __attribute__((always_inline)) -> unsigned long long { return 1; }, (unsigned long long)k, from);
-    }
-  }
-  if (cut_p && listed) {
-    const double run = list_sums(listed), before = run - (tid < listed ? shares[tid] : 0.0);
-    __syncthreads();
-    if (tid == kept_list - 1) found.total = run;
-    __syncthreads();
-    const double need = p * found.total;
-    // the first element at which the sum reaches `need`: those whose sum in front of them does not are kept, the first always
-    kept_list = (int)block_sum(tid < kept_list && (tid == 0 || before < need) ? 1ull : 0ull);
-  } else if (cut_p) {
-    // whole row (or what a long top-k has left): its mass, then the list if it holds enough of it
-    double mass = 0.0;
-    each([&](int, const float(&x)[VEC], int i0) __attribute__((always_inline)) {
-#pragma unroll
-      for (int c = 0; c < VEC; ++c)
-        if (kept(x[c], i0 + c)) mass += energy(x[c]);
-    });
-    mass = block_fold(mass, take_sum<double>) / (64 / kWaves);
-    const double need = p * mass;
-    const int n = list_from(fmaxf(floor_of(kMaxima), cut_x));
-    bool enough = false;
-    if (n <= kList) {
-      const bool mine = tid < n && kept(of_ordered(~(uint32_t)(keys[tid < n ? tid : 0] >> 32)), (int)(uint32_t)keys[tid < n ? tid : 0]);
-      const double run = list_sums(n), before = run - (tid < n ? shares[tid] : 0.0);
-      const int m = (int)block_sum(mine && (tid == 0 || before < need) ? 1ull : 0ull);
-      __syncthreads();
-      if (tid == n - 1) found.total = run;
-      __syncthreads();
-      enough = m < n || found.total >= need;
-      if (enough) listed = n, kept_list = m;
-    }
-    if (!enough) {
-      const double whole_need = ceil(need * 8796093022208.0);          // 2^43
-      search(whole, whole_need >= 1.0 ? (unsigned long long)whole_need : 1ull, -INFINITY);
-    }
-  }
-  if (listed && least > 0.0) kept_list = (int)block_sum(tid < kept_list && shares[tid] >= least ? 1ull : 0ull);
   const float u_in = a.u[row];
   const double u = u_in > 0.f ? (double)u_in : 0.0;
-  if (listed && kept_list <= 64) {
-    // few are kept: one wavefront holds them, brings them into the order of their indices and adds up
+  int kept_list = 0;                                       // elements of the list that are kept; 0: no list
+  __syncthreads();                                         // (the table of roots)
+  if (k) {
+    const float from = k <= kThreads ? floor_of(k) : -INFINITY;
+    const int n = k <= kList / 2 || V <= kList ? list_from(from) : kList + 1;
+    if (n <= kList) {
+      kept_list = k < n ? k : n;
+    } else {
+      low = block_fold(low, INFINITY, smaller);
+      search([](float) __attribute__((always_inline)) -> unsigned long long { return 1; }, (unsigned long long)k, -1.0, fmaxf(from, low), top);
+    }
+  }
+  if (cut_p && kept_list) {
+    const double mine = tid < kept_list ? shares[tid] : 0.0, run = block_run(mine, 0.0);
+    if (tid == kThreads - 1) found.total = run;
+    __syncthreads();
+    // those whose sum in front of them does not reach p are kept, the first always
+    kept_list = count(tid < kept_list && (tid == 0 || run - mine < p * found.total));
+  } else if (cut_p) {
+    if (!k) low = block_fold(low, INFINITY, smaller);
+    // (32 temperatures below the maximum an element weighs less than half of 2^-43: nothing)
+    search(whole, 0, p, fmaxf(fmaxf(cut_x, low), top - 32.0f * temp), top);
+  }
+  if (kept_list && least > 0.0) kept_list = count(tid < kept_list && shares[tid] >= least);
+  if (kept_list && kept_list <= kShort) {
+    // few are kept: brought into the order of their indices, four threads counting for an element, and one wavefront adds up
+    const int who = tid >> 2, part = tid & 3;
+    const uint32_t index = who < kept_list ? (uint32_t)keys[who] : 0;
+    int rank = 0;
+    for (int o = part; o < kept_list; o += 4) rank += (uint32_t)keys[o] < index;
+    rank += __shfl_xor(rank, 1, 64);
+    rank += __shfl_xor(rank, 2, 64);
+    __syncthreads();
+    if (who < kept_list && part == 0) by_index[rank] = index, by_index_e[rank] = shares[who];
+    __syncthreads();
     if (wave) return;
-    uint32_t index = lane < kept_list ? (uint32_t)keys[lane] : 0xffffffffu;
-    double e = lane < kept_list ? shares[lane] : 0.0;
+    constexpr int PER = kShort / 64;
+    double e[PER], sum = 0.0;
 #pragma unroll
-    for (int half = 2; half <= 64; half *= 2)
+    for (int i = 0; i < PER; ++i) sum += e[i] = PER * lane + i < kept_list ? by_index_e[PER * lane + i] : 0.0;
+    const double run = wave_run(sum, 0.0, add), total = lane_of(run, 63), target = u * total;
+    const unsigned long long past = __ballot(sum > 0.0 && run > target), some = __ballot(sum > 0.0);
+    if (lane != (past ? __builtin_ctzll(past) : 63 - __builtin_clzll(some))) return;
+    double cum = run - sum, mine = 0.0;
+    int at = 0;
+    bool done = false;
 #pragma unroll
-      for (int stride = half / 2; stride; stride /= 2) {
-        const uint32_t other = __shfl_xor(index, stride, 64);
-        const double other_e = __shfl_xor(e, stride, 64);
-        const bool up = (lane & half) == 0, first = (lane & stride) == 0;
-        const bool take = (other < index) == (up == first) && other != index;
-        index = take ? other : index, e = take ? other_e : e;
-      }
-    double run = e;
-    for (int o = 1; o < 64; o <<= 1) {
-      const double other = __shfl_up(run, o, 64);
-      if (lane >= o) run += other;
+    for (int i = 0; i < PER; ++i) {
+      cum += e[i];
+      if (!done && e[i] > 0.0) at = PER * lane + i, mine = e[i], done = cum > target;
     }
-    const double total = __shfl(run, 63, 64), target = u * total;
-    const unsigned long long past = __ballot(e > 0.0 && run > target), some = __ballot(e > 0.0);
-    const int who = past ? __builtin_ctzll(past) : 63 - __builtin_clzll(some);
-    if (lane == who) {
-      a.tokens[row] = (int)index;
-      if (a.logprob) a.logprob[row] = (float)log(e / total);
-    }
+    a.tokens[row] = (int)by_index[at];
+    if (a.logprob) a.logprob[row] = (float)log(mine / total);
     return;
   }
-  if (listed) {
-    __syncthreads();
-    cut_at(kept_list - 1);
-  }
+  if (kept_list) cut_x = of_ordered(~(uint32_t)(keys[kept_list - 1] >> 32)), cut_i = (int)(uint32_t)keys[kept_list - 1];
   // min-p: what lies well below its border by value is not worth an exponential
   if (least > 0.0) {
     const float near = nextafterf((float)((double)top + (double)temp * (log(least) - 1e-3)), -INFINITY);
@@ -479,18 +507,29 @@ __global__ __launch_bounds__(kThreads) void sample_rows_kernel(SampleRows a) {
   }
 
   // draw: sums of 64 x VEC consecutive elements, then of the segments, then inside the one that u falls into
-  auto drawn = [&](float x, int i) __attribute__((always_inline)) -> double {
-    if (!kept(x, i)) return 0.0;
-    const double e = energy(x);
-    return e >= least ? e : 0.0;
+  auto drawn = [&](const float(&x)[VEC], int i0, double(&e)[VEC]) __attribute__((always_inline)) -> double {
+    bool some = false;
+#pragma unroll
+    for (int c = 0; c < VEC; ++c) some |= kept(x[c], i0 + c);
+    double sum = 0.0;
+    if (!__any(some)) {
+#pragma unroll
+      for (int c = 0; c < VEC; ++c) e[c] = 0.0;
+      return sum;
+    }
+#pragma unroll
+    for (int c = 0; c < VEC; ++c) {
+      e[c] = energy(x[c]);
+      e[c] = kept(x[c], i0 + c) && e[c] >= least ? e[c] : 0.0;
+      sum += e[c];
+    }
+    return sum;
   };
   __syncthreads();
   each([&](int j, const float(&x)[VEC], int i0) __attribute__((always_inline)) {
-    double sum = 0.0;
-#pragma unroll
-    for (int c = 0; c < VEC; ++c) sum += drawn(x[c], i0 + c);
-    sum = wave_fold<double>(sum, take_sum<double>);
-    if (lane == 0) segs[j * kWaves + wave] = sum;
+    double e[VEC];
+    const double sum = wave_run(drawn(x, i0, e), 0.0, add);
+    if (lane == 63) segs[j * kWaves + wave] = sum;
   });
   __syncthreads();
   const int n_segs = chunks * kWaves;
@@ -498,18 +537,12 @@ __global__ __launch_bounds__(kThreads) void sample_rows_kernel(SampleRows a) {
     const int per = (n_segs + 63) / 64, s0 = lane * per, s1 = s0 + per < n_segs ? s0 + per : n_segs;
     double sum = 0.0;
     for (int s = s0; s < s1; ++s) sum += segs[s];
-    double run = sum;
-    for (int o = 1; o < 64; o <<= 1) {
-      const double other = __shfl_up(run, o, 64);
-      if (lane >= o) run += other;
-    }
-    const double total = __shfl(run, 63, 64), target = u * total;
+    const double run = wave_run(sum, 0.0, add), total = lane_of(run, 63), target = u * total;
     const unsigned long long past = __ballot(run > target), some = __ballot(sum > 0.0);
     const int who = past ? __builtin_ctzll(past) : 63 - __builtin_clzll(some);
     if (lane == who) {
-      double before = run - sum;
+      double before = run - sum, at = 0.0;
       int seg = -1;
-      double at = 0.0;
       for (int s = s0; s < s1; ++s) {
         if (segs[s] > 0.0) {
           seg = s, at = before;
@@ -529,15 +562,8 @@ __global__ __launch_bounds__(kThreads) void sample_rows_kernel(SampleRows a) {
     float x[VEC];
 #pragma unroll
     for (int c = 0; c < VEC; ++c) x[c] = plain(value_of<T>(w, c));
-    double e[VEC], sum = 0.0;
-#pragma unroll
-    for (int c = 0; c < VEC; ++c) sum += e[c] = drawn(x[c], i0 + c);
-    double run = sum;
-    for (int o = 1; o < 64; o <<= 1) {
-      const double other = __shfl_up(run, o, 64);
-      if (lane >= o) run += other;
-    }
-    const double target = u * found.total;
+    double e[VEC];
+    const double sum = drawn(x, i0, e), run = wave_run(sum, 0.0, add), target = u * found.total;
     const unsigned long long past = __ballot(sum > 0.0 && found.before + run > target), some = __ballot(sum > 0.0);
     const int who = past ? __builtin_ctzll(past) : 63 - __builtin_clzll(some);
     if (lane != who) return;
