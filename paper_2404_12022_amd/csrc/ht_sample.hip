@@ -24,6 +24,8 @@ namespace ht {
 namespace {
 
 constexpr int kThreads = 1024, kWaves = kThreads / 64, kBins = 2048, kList = 1024;
+constexpr int kRoots = 32;                   // as many as fill the banks of LDS once: lanes on different entries do not conflict
+constexpr double kNothing = 1e-300;          // e up to here is an exponential's zero
 constexpr int kShort = 256;                  // list lengths whose order is counted out, not sorted: a sort's steps wait for each other
 
 template <typename T> struct Vec16;
@@ -49,7 +51,6 @@ struct Found {
   unsigned long long above;                  // search: weight above the crossing step
   uint32_t lo, hi;                           // search: its elements' range, as ordered keys
   int32_t bin, listed, index, seg;
-  float value;
 };
 
 __device__ inline uint32_t ordered(float v) {
@@ -105,6 +106,20 @@ template <typename V, typename F> __device__ inline V row_run(V v, V none, F f) 
   return v;
 }
 
+// lower half: a there plus a 32 lanes on, upper half: the same of b; and with rows of 16, odd rows of b
+__device__ inline double fold_halves(double a, double b) {
+  const uint64_t x = __builtin_bit_cast(uint64_t, a), y = __builtin_bit_cast(uint64_t, b);
+  const auto lo = __builtin_amdgcn_permlane32_swap((uint32_t)x, (uint32_t)y, false, false);
+  const auto hi = __builtin_amdgcn_permlane32_swap((uint32_t)(x >> 32), (uint32_t)(y >> 32), false, false);
+  return __builtin_bit_cast(double, (uint64_t)hi[0] << 32 | lo[0]) + __builtin_bit_cast(double, (uint64_t)hi[1] << 32 | lo[1]);
+}
+__device__ inline double fold_rows(double a, double b) {
+  const uint64_t x = __builtin_bit_cast(uint64_t, a), y = __builtin_bit_cast(uint64_t, b);
+  const auto lo = __builtin_amdgcn_permlane16_swap((uint32_t)x, (uint32_t)y, false, false);
+  const auto hi = __builtin_amdgcn_permlane16_swap((uint32_t)(x >> 32), (uint32_t)(y >> 32), false, false);
+  return __builtin_bit_cast(double, (uint64_t)hi[0] << 32 | lo[0]) + __builtin_bit_cast(double, (uint64_t)hi[1] << 32 | lo[1]);
+}
+
 }  // namespace
 
 template <typename T>
@@ -113,16 +128,13 @@ __global__ __launch_bounds__(kThreads) void sample_rows_kernel(SampleRows a) {
   // histogram and list of the search, or the segment sums of the draw
   __shared__ __attribute__((aligned(16))) unsigned char shared_mem[32768];
   unsigned long long* hist = (unsigned long long*)shared_mem;                    // [kBins]
-  unsigned long long* list_w = (unsigned long long*)(shared_mem + 16384);        // [kList]
-  float* list_x = (float*)(shared_mem + 24576);                                  // [kList]
-  int32_t* list_i = (int32_t*)(shared_mem + 28672);                              // [kList]
   double* segs = (double*)shared_mem;                                            // [4096]
   unsigned long long* loose = (unsigned long long*)(shared_mem + 16384);         // [kList] the list before it is sorted
   uint32_t* by_index = (uint32_t*)(shared_mem + 8192);                           // [kShort] the kept ones in the order of their indices
   double* by_index_e = (double*)shared_mem;
   __shared__ unsigned long long keys[kList];                                     // the sorted list: order, then index
   __shared__ double shares[kList];                                               // ... and its e
-  __shared__ double roots[32];                                                   // 2^(j / 32)
+  __shared__ double roots[kRoots];                                               // 2^(j / kRoots)
   __shared__ unsigned long long fold[2][kWaves];
   __shared__ Found found;
 
@@ -131,11 +143,7 @@ __global__ __launch_bounds__(kThreads) void sample_rows_kernel(SampleRows a) {
   const int chunks = (V + STRIDE - 1) / STRIDE;
   bool spike = false;                                      // the maximum is +inf: those tokens share everything
 
-  // NaN counts as -inf, -0 ties with 0
-  auto plain = [&](float v) __attribute__((always_inline)) {
-    v = v == v ? v + 0.0f : -INFINITY;
-    return !spike ? v : v == INFINITY ? 0.f : -INFINITY;
-  };
+  auto plain = [&](float v) __attribute__((always_inline)) { return v == v ? v : -INFINITY; };       // NaN counts as -inf
   auto piece = [&](uint32_t (&w)[4], int j) __attribute__((always_inline)) {
     const int i0 = (j * kThreads + tid) * VEC;
     if (i0 + VEC <= V) {
@@ -149,6 +157,16 @@ __global__ __launch_bounds__(kThreads) void sample_rows_kernel(SampleRows a) {
         if (i0 + c < V) raw[c] = z[i0 + c];
       }
       __builtin_memcpy(w, raw, 16);
+    }
+    if (spike) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        if (sizeof(T) == 4) {
+          w[i] = w[i] == 0x7f800000u ? 0u : 0xff800000u;
+        } else {
+          w[i] = ((w[i] & 0xffffu) == 0x7f80u ? 0u : 0xff80u) | (w[i] >> 16 == 0x7f80u ? 0u : 0xff800000u);
+        }
+      }
     }
   };
   // f(chunk, values, first index), AHEAD pieces on their way at a time
@@ -196,7 +214,7 @@ __global__ __launch_bounds__(kThreads) void sample_rows_kernel(SampleRows a) {
     return wave ? v + lane_of(ends, wave - 1) : v;
   };
 
-  if (tid < 32) roots[tid] = tid ? 2.0 * exp_series((tid - 32) * (0.69314718055994531 / 32.0)) : 1.0;
+  if (tid < kRoots) roots[tid] = tid ? 2.0 * exp_series((tid - kRoots) * (0.69314718055994531 / kRoots)) : 1.0;
   float best = -INFINITY, low = INFINITY;                  // this thread's largest value, the smallest one
   each([&](int, const float(&x)[VEC], int) __attribute__((always_inline)) {
 #pragma unroll
@@ -235,16 +253,19 @@ __global__ __launch_bounds__(kThreads) void sample_rows_kernel(SampleRows a) {
     top = low = 0.f;
   }
   // e = 2^(y / 32), y = 32 (x - top) / (T ln 2) = n + f, |f| <= 1/2: a table for n modulo 32, a power of two, and the series of 2^(f / 32) to
-  // f^5 (the first term left out is 2e-15).  y is 0 at the maximum and e is 1.  12 operations in 64 bits; with the series of the whole
-  // exponential (20) the pass over 32000 values of one row took 16 us
-  const double steepness = 46.166241308446828 / (double)temp;          // 32 / ln 2
+  // f^5 (the first term left out is 2e-15).  y is 0 at the maximum and e is 1.  With the series of the whole exponential
+  // to f^13 the pass over 32000 values of one row took 16 us, now 10
+  const double steepness = kRoots / 0.69314718055994531 / (double)temp;
   auto energy = [&](float x) __attribute__((always_inline)) -> double {
-    constexpr double s = 0.69314718055994531 / 32.0, c1 = s, c2 = s * s / 2, c3 = s * s * s / 6, c4 = s * s * s * s / 24, c5 = s * s * s * s * s / 120;
-    const double y = fmax(((double)x - (double)top) * steepness, -60000.0);      // (-inf, and its product with 0: e is 0)
-    const double n = rint(y), f = y - n;
-    const int k = (int)n;
-    const double p = f * fma(f, fma(f, fma(f, fma(f, c5, c4), c3), c2), c1), root = roots[k & 31];
-    return ldexp(fma(root, p, root), k >> 5);
+    constexpr double c1 = 0.69314718055994531 / kRoots, c2 = c1 * c1 / 2, c3 = c1 * c1 * c1 / 6, c4 = c2 * c2 / 6, c5 = c2 * c3 / 10;
+    // n as the low bits of y + 1.5 2^52, and the power of two added to the exponent: rounding, conversion and ldexp are slow instructions
+    // n as the low bits of y + 1.5 2^52, and the power of two added to the exponent: a pass is bound by the instructions it issues.
+    // Below 2^-1020 (at -inf too) e stays there, which no sum notices (kNothing)
+    const double y = fmax(((double)x - (double)top) * steepness, -32.0 * 1020.0), t = y + 6755399441055744.0, f = y - (t - 6755399441055744.0);
+    const uint32_t k = (uint32_t)__builtin_bit_cast(uint64_t, t);
+    const double root = roots[k & (kRoots - 1)], e = fma(root, f * fma(f, fma(f, fma(f, fma(f, c5, c4), c3), c2), c1), root);
+    const uint64_t bits = __builtin_bit_cast(uint64_t, e);
+    return __builtin_bit_cast(double, (uint64_t)((uint32_t)(bits >> 32) + ((k & ~31u) << 15)) << 32 | (uint32_t)bits);
   };
   // in whole 2^-43, up to 2^20 of them in 64 bits: the mantissa's end of e + 512
   auto whole = [&](float x) __attribute__((always_inline)) -> unsigned long long {
@@ -253,7 +274,57 @@ __global__ __launch_bounds__(kThreads) void sample_rows_kernel(SampleRows a) {
 
   float cut_x = -INFINITY;                                 // kept so far: what comes before or is (cut_x, cut_i)
   int cut_i = -1;
-  auto kept = [&](float x, int i) __attribute__((always_inline)) { return x > cut_x || (x == cut_x && i <= cut_i); };
+  auto kept = [&](float x, int i) __attribute__((always_inline)) { return (x > cut_x) | ((x == cut_x) & (i <= cut_i)); };
+
+  // `loose` (n of them) into `keys`, ascending, with their e
+  auto sort_list = [&](int n) __attribute__((always_inline)) {
+    if (n <= kShort) {
+      // four threads count a quarter of the list each for an element
+      const int who = tid >> 2, part = tid & 3, whole_n = (n + 31) & ~31;
+      if (tid >= n && tid < whole_n) loose[tid] = ~0ull;
+      __syncthreads();
+      const unsigned long long key = who < n ? loose[who] : 0;
+      int rank = 0;
+      for (int o = part; o < whole_n; o += 32) {
+#pragma unroll
+        for (int i = 0; i < 32; i += 4) rank += loose[o + i] < key;
+      }
+      rank += __shfl_xor(rank, 1, 64);
+      rank += __shfl_xor(rank, 2, 64);
+      if (who < n && part == 0) {
+        keys[rank] = key;
+        shares[rank] = energy(of_ordered(~(uint32_t)(key >> 32)));
+      }
+    } else {
+      // bitonic, strides below 64 inside a wavefront
+      int size = 512;
+      while (size < n) size *= 2;
+      unsigned long long key = tid < n ? loose[tid] : ~0ull;
+      for (int half = 2; half <= size; half *= 2)
+        for (int stride = half / 2; stride; stride /= 2) {
+          unsigned long long other;
+          if (stride >= 64) {
+            __syncthreads();
+            if (tid < size) keys[tid] = key;
+            __syncthreads();
+            other = tid < size ? keys[tid ^ stride] : 0;
+          } else {
+            if (wave * 64 >= size) continue;
+            other = __shfl_xor(key, stride, 64);
+          }
+          const bool up = (tid & half) == 0, first = (tid & stride) == 0;
+          key = (other < key) == (up == first) ? other : key;
+        }
+      __syncthreads();
+      if (tid < size) keys[tid] = key;
+      if (tid < n) shares[tid] = energy(of_ordered(~(uint32_t)(key >> 32)));
+    }
+    __syncthreads();
+  };
+  auto key_of = [&](float x, int i) __attribute__((always_inline)) { return (unsigned long long)~ordered(x + 0.0f) << 32 | (uint32_t)i; };      // (-0 ties with 0)
+  auto cut_at = [&](int i) __attribute__((always_inline)) {
+    cut_x = of_ordered(~(uint32_t)(keys[i] >> 32)), cut_i = (int)(uint32_t)keys[i];
+  };
 
   // the element of the kept ones at which the running weight reaches `need` (at least 1), or a share of all the weight from lo on where
   // `share` is not negative, becomes the cut; none if it never does.  Elements above hi or below lo are left alone
@@ -291,17 +362,24 @@ __global__ __launch_bounds__(kThreads) void sample_rows_kernel(SampleRows a) {
       if (tid == 0) found.bin = -1, found.listed = 0, found.lo = 0xffffffffu, found.hi = 0;
       __syncthreads();
       const double steps = kBins / ((double)hi - (double)lo);
-      auto bin_of = [&](float x) __attribute__((always_inline)) {
+      auto bin_of = [&](float x) __attribute__((always_inline)) {           // (of any x: within the bins)
         const int n = (int)(((double)hi - (double)x) * steps);
-        return n < kBins ? n : kBins - 1;
+        return n < 0 ? 0 : n < kBins ? n : kBins - 1;
       };
       each([&](int, const float(&x)[VEC], int i0) __attribute__((always_inline)) {
+        bool in[VEC], some = false;
+#pragma unroll
+        for (int c = 0; c < VEC; ++c) some |= in[c] = (x[c] >= lo) & (x[c] <= hi) & kept(x[c], i0 + c);
+        if (!__any(some)) return;
+        unsigned long long w[VEC];
+        int bin[VEC];
+#pragma unroll
+        for (int c = 0; c < VEC; ++c) w[c] = weight(x[c]), bin[c] = bin_of(x[c]);
+#pragma unroll
+        for (int c = 0; c < VEC; ++c) asm volatile("" : "+v"(w[c]), "+v"(bin[c]));
 #pragma unroll
         for (int c = 0; c < VEC; ++c)
-          if (x[c] >= lo && x[c] <= hi && kept(x[c], i0 + c)) {
-            const unsigned long long w = weight(x[c]);
-            if (w) atomicAdd(&hist[bin_of(x[c])], w);
-          }
+          if (in[c] && w[c]) atomicAdd(&hist[bin[c]], w[c]);
       });
       __syncthreads();
       const unsigned long long h0 = hist[2 * tid], h1 = hist[2 * tid + 1];       // two steps a thread
@@ -321,18 +399,16 @@ __global__ __launch_bounds__(kThreads) void sample_rows_kernel(SampleRows a) {
       const int bin = found.bin;
       if (bin < 0) return;
       above = found.above;
+      // its elements; a range of values a step wider on either side spares the others the 64-bit arithmetic
+      const float wide_hi = (float)((double)hi - (bin - 1) / steps), wide_lo = bin == kBins - 1 ? lo : (float)((double)hi - (bin + 2) / steps);
       each([&](int, const float(&x)[VEC], int i0) __attribute__((always_inline)) {
 #pragma unroll
         for (int c = 0; c < VEC; ++c)
-          if (x[c] >= lo && x[c] <= hi && bin_of(x[c]) == bin && kept(x[c], i0 + c)) {
+          if (x[c] >= wide_lo && x[c] <= wide_hi && x[c] >= lo && x[c] <= hi && bin_of(x[c]) == bin && kept(x[c], i0 + c)) {
             const int at = atomicAdd(&found.listed, 1);
-            if (at < kList) {
-              list_x[at] = x[c];
-              list_i[at] = i0 + c;
-              list_w[at] = weight(x[c]);
-            }
-            atomicMin(&found.lo, ordered(x[c]));
-            atomicMax(&found.hi, ordered(x[c]));
+            if (at < kList) loose[at] = key_of(x[c], i0 + c);
+            atomicMin(&found.lo, ordered(x[c] + 0.0f));
+            atomicMax(&found.hi, ordered(x[c] + 0.0f));
           }
       });
       __syncthreads();
@@ -341,15 +417,11 @@ __global__ __launch_bounds__(kThreads) void sample_rows_kernel(SampleRows a) {
         lo = of_ordered(found.lo), hi = of_ordered(found.hi);
         continue;
       }
-      if (tid < n) {
-        const float x = list_x[tid];
-        const int i = list_i[tid];
-        unsigned long long front = above;
-        for (int o = 0; o < n; ++o) front += list_x[o] > x || (list_x[o] == x && list_i[o] < i) ? list_w[o] : 0;
-        if (front < need && front + list_w[tid] >= need) found.value = x, found.index = i;
-      }
+      sort_list(n);
+      const unsigned long long w = tid < n ? weight(of_ordered(~(uint32_t)(keys[tid] >> 32))) : 0, up_to = above + block_run(w, 0ull);
+      if (up_to - w < need && up_to >= need) found.index = tid;
       __syncthreads();
-      cut_x = found.value, cut_i = found.index;
+      cut_at(found.index);
       return;
     }
   };
@@ -390,49 +462,13 @@ __global__ __launch_bounds__(kThreads) void sample_rows_kernel(SampleRows a) {
         for (int c = 0; c < VEC; ++c)
           if (x[c] >= from && x[c] > -INFINITY) {
             const int at = atomicAdd(&found.listed, 1);
-            if (at < kList) loose[at] = (unsigned long long)~ordered(x[c]) << 32 | (uint32_t)(i0 + c);
+            if (at < kList) loose[at] = key_of(x[c], i0 + c);
           }
       });
     __syncthreads();
     const int n = found.listed;
     if (n > kList) return n;
-    if (n <= kShort) {
-      // four threads count a quarter of the list each for an element
-      const int who = tid >> 2, part = tid & 3;
-      const unsigned long long key = who < n ? loose[who] : 0;
-      int rank = 0;
-      for (int o = part; o < n; o += 4) rank += loose[o] < key;
-      rank += __shfl_xor(rank, 1, 64);
-      rank += __shfl_xor(rank, 2, 64);
-      if (who < n && part == 0) {
-        keys[rank] = key;
-        shares[rank] = energy(of_ordered(~(uint32_t)(key >> 32)));
-      }
-    } else {
-      // bitonic, strides below 64 inside a wavefront
-      int size = 512;
-      while (size < n) size *= 2;
-      unsigned long long key = tid < n ? loose[tid] : ~0ull;
-      for (int half = 2; half <= size; half *= 2)
-        for (int stride = half / 2; stride; stride /= 2) {
-          unsigned long long other;
-          if (stride >= 64) {
-            __syncthreads();
-            if (tid < size) keys[tid] = key;
-            __syncthreads();
-            other = tid < size ? keys[tid ^ stride] : 0;
-          } else {
-            if (wave * 64 >= size) continue;
-            other = __shfl_xor(key, stride, 64);
-          }
-          const bool up = (tid & half) == 0, first = (tid & stride) == 0;
-          key = (other < key) == (up == first) ? other : key;
-        }
-      __syncthreads();
-      if (tid < size) keys[tid] = key;
-      if (tid < n) shares[tid] = energy(of_ordered(~(uint32_t)(key >> 32)));
-    }
-    __syncthreads();
+    sort_list(n);
     return n;
   };
 
@@ -473,7 +509,10 @@ __global__ __launch_bounds__(kThreads) void sample_rows_kernel(SampleRows a) {
     const int who = tid >> 2, part = tid & 3;
     const uint32_t index = who < kept_list ? (uint32_t)keys[who] : 0;
     int rank = 0;
-    for (int o = part; o < kept_list; o += 4) rank += (uint32_t)keys[o] < index;
+    for (int o = part; o < kept_list; o += 32) {
+#pragma unroll
+      for (int i = 0; i < 32; i += 4) rank += o + i < kept_list && (uint32_t)keys[o + i] < index;
+    }
     rank += __shfl_xor(rank, 1, 64);
     rank += __shfl_xor(rank, 2, 64);
     __syncthreads();
@@ -485,7 +524,7 @@ __global__ __launch_bounds__(kThreads) void sample_rows_kernel(SampleRows a) {
 #pragma unroll
     for (int i = 0; i < PER; ++i) sum += e[i] = PER * lane + i < kept_list ? by_index_e[PER * lane + i] : 0.0;
     const double run = wave_run(sum, 0.0, add), total = lane_of(run, 63), target = u * total;
-    const unsigned long long past = __ballot(sum > 0.0 && run > target), some = __ballot(sum > 0.0);
+    const unsigned long long past = __ballot(sum > kNothing && run > target), some = __ballot(sum > kNothing);
     if (lane != (past ? __builtin_ctzll(past) : 63 - __builtin_clzll(some))) return;
     double cum = run - sum, mine = 0.0;
     int at = 0;
@@ -493,13 +532,13 @@ __global__ __launch_bounds__(kThreads) void sample_rows_kernel(SampleRows a) {
 #pragma unroll
     for (int i = 0; i < PER; ++i) {
       cum += e[i];
-      if (!done && e[i] > 0.0) at = PER * lane + i, mine = e[i], done = cum > target;
+      if (!done && e[i] > kNothing) at = PER * lane + i, mine = e[i], done = cum > target;
     }
     a.tokens[row] = (int)by_index[at];
     if (a.logprob) a.logprob[row] = (float)log(mine / total);
     return;
   }
-  if (kept_list) cut_x = of_ordered(~(uint32_t)(keys[kept_list - 1] >> 32)), cut_i = (int)(uint32_t)keys[kept_list - 1];
+  if (kept_list) cut_at(kept_list - 1);
   // min-p: what lies well below its border by value is not worth an exponential
   if (least > 0.0) {
     const float near = nextafterf((float)((double)top + (double)temp * (log(least) - 1e-3)), -INFINITY);
@@ -507,30 +546,60 @@ __global__ __launch_bounds__(kThreads) void sample_rows_kernel(SampleRows a) {
   }
 
   // draw: sums of 64 x VEC consecutive elements, then of the segments, then inside the one that u falls into
+  const bool all = cut_x == -INFINITY && least <= 0.0;
   auto drawn = [&](const float(&x)[VEC], int i0, double(&e)[VEC]) __attribute__((always_inline)) -> double {
-    bool some = false;
-#pragma unroll
-    for (int c = 0; c < VEC; ++c) some |= kept(x[c], i0 + c);
     double sum = 0.0;
-    if (!__any(some)) {
+    if (!all) {
+      bool some = false;
 #pragma unroll
-      for (int c = 0; c < VEC; ++c) e[c] = 0.0;
-      return sum;
+      for (int c = 0; c < VEC; ++c) some |= kept(x[c], i0 + c);
+      if (!__any(some)) {
+#pragma unroll
+        for (int c = 0; c < VEC; ++c) e[c] = 0.0;
+        return sum;
+      }
+    }
+    // all of them, side by side: the compiler would put every exponential into a branch of its own, one latency after the other
+#pragma unroll
+    for (int c = 0; c < VEC; ++c) e[c] = energy(x[c]);
+#pragma unroll
+    for (int c = 0; c < VEC; ++c) asm volatile("" : "+v"(e[c]));
+    if (!all) {
+#pragma unroll
+      for (int c = 0; c < VEC; ++c) e[c] = kept(x[c], i0 + c) & (e[c] >= least) ? e[c] : 0.0;
     }
 #pragma unroll
-    for (int c = 0; c < VEC; ++c) {
-      e[c] = energy(x[c]);
-      e[c] = kept(x[c], i0 + c) && e[c] >= least ? e[c] : 0.0;
-      sum += e[c];
-    }
+    for (int c = 0; c < VEC; ++c) sum += e[c];
     return sum;
   };
   __syncthreads();
-  each([&](int j, const float(&x)[VEC], int i0) __attribute__((always_inline)) {
-    double e[VEC];
-    const double sum = wave_run(drawn(x, i0, e), 0.0, add);
-    if (lane == 63) segs[j * kWaves + wave] = sum;
-  });
+#pragma unroll 1
+  for (int j0 = 0; j0 < chunks; j0 += AHEAD) {
+    uint32_t w[AHEAD][4];
+#pragma unroll
+    for (int i = 0; i < AHEAD; ++i)
+      if (j0 + i < chunks) piece(w[i], j0 + i);
+    double s[AHEAD];
+#pragma unroll
+    for (int i = 0; i < AHEAD; ++i) {
+      s[i] = 0.0;
+      if (j0 + i < chunks) {
+        float x[VEC];
+#pragma unroll
+        for (int c = 0; c < VEC; ++c) x[c] = plain(value_of<T>(w[i], c));
+        double e[VEC];
+        s[i] = drawn(x, ((j0 + i) * kThreads + tid) * VEC, e);
+      }
+    }
+    // four wavefront sums together: halves and rows of sixteen change places between them, and what is left is one sum over 16 lanes
+    static_assert(AHEAD == 4, "four at a time");
+    const double a01 = fold_halves(s[0], s[1]), a23 = fold_halves(s[2], s[3]);             // lower half: of 0 and 2, upper of 1 and 3
+    const double sums = row_run(fold_rows(a01, a23), 0.0, add);                            // rows of 16: 0, 2, 1, 3
+    if ((lane & 15) == 15) {
+      const int i = (lane >> 5) | (lane >> 4 & 1) << 1;
+      if (j0 + i < chunks) segs[(j0 + i) * kWaves + wave] = sums;
+    }
+  }
   __syncthreads();
   const int n_segs = chunks * kWaves;
   if (wave == 0) {
@@ -538,13 +607,13 @@ __global__ __launch_bounds__(kThreads) void sample_rows_kernel(SampleRows a) {
     double sum = 0.0;
     for (int s = s0; s < s1; ++s) sum += segs[s];
     const double run = wave_run(sum, 0.0, add), total = lane_of(run, 63), target = u * total;
-    const unsigned long long past = __ballot(run > target), some = __ballot(sum > 0.0);
+    const unsigned long long past = __ballot(sum > kNothing && run > target), some = __ballot(sum > kNothing);
     const int who = past ? __builtin_ctzll(past) : 63 - __builtin_clzll(some);
     if (lane == who) {
       double before = run - sum, at = 0.0;
       int seg = -1;
       for (int s = s0; s < s1; ++s) {
-        if (segs[s] > 0.0) {
+        if (segs[s] > kNothing) {
           seg = s, at = before;
           if (before + segs[s] > target) break;
         }
@@ -564,7 +633,7 @@ __global__ __launch_bounds__(kThreads) void sample_rows_kernel(SampleRows a) {
     for (int c = 0; c < VEC; ++c) x[c] = plain(value_of<T>(w, c));
     double e[VEC];
     const double sum = drawn(x, i0, e), run = wave_run(sum, 0.0, add), target = u * found.total;
-    const unsigned long long past = __ballot(sum > 0.0 && found.before + run > target), some = __ballot(sum > 0.0);
+    const unsigned long long past = __ballot(sum > kNothing && found.before + run > target), some = __ballot(sum > kNothing);
     const int who = past ? __builtin_ctzll(past) : 63 - __builtin_clzll(some);
     if (lane != who) return;
     double cum = found.before + run - sum, mine = 0.0;
@@ -573,7 +642,7 @@ __global__ __launch_bounds__(kThreads) void sample_rows_kernel(SampleRows a) {
 #pragma unroll
     for (int c = 0; c < VEC; ++c) {
       cum += e[c];
-      if (!done && e[c] > 0.0) {
+      if (!done && e[c] > kNothing) {
         token = i0 + c, mine = e[c];
         done = cum > target;
       }
