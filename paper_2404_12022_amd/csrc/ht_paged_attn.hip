@@ -101,6 +101,16 @@ struct __attribute__((packed, aligned(2))) Loose8 {
   uint2 v;
 };
 
+// Four outputs, over their sum (0 over an empty one)
+__device__ __forceinline__ void store_four(bf16_t* out, const floatx4_t& acc, float sum) {
+  const float inv = sum == 0.f ? 0.f : 1.0f / sum;
+  ((Loose8*)out)->v = sum == 0.f ? make_uint2(0, 0) : pack4_bf16(acc[0] * inv, acc[1] * inv, acc[2] * inv, acc[3] * inv);
+}
+__device__ __forceinline__ void store_four(float* out, const floatx4_t& acc, float sum) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i) out[i] = sum == 0.f ? 0.f : acc[i] / sum;
+}
+
 constexpr float kRescaleStep = 8.0f;         // log2 units the reference point may lag behind the maximum: probabilities stay below 2^8
 
 __device__ __forceinline__ float max_over_groups(float x) {
@@ -431,9 +441,7 @@ template <int HD, int QB> struct Columns {
     if (part_o) {
       *(float4*)(part_o + (at * a.Hq + head[qb]) * HD + e0) = make_float4(acc[0], acc[1], acc[2], acc[3]);
     } else {
-      const float inv = sum == 0.f ? 0.f : 1.0f / sum;
-      ((Loose8*)((bf16_t*)a.out + at * a.out_stride + (int64_t)head[qb] * HD + e0))->v =
-          sum == 0.f ? make_uint2(0, 0) : pack4_bf16(acc[0] * inv, acc[1] * inv, acc[2] * inv, acc[3] * inv);
+      store_four((bf16_t*)a.out + at * a.out_stride + (int64_t)head[qb] * HD + e0, acc, sum);
     }
   }
   __device__ __forceinline__ void finish_sum(const AttnRows& a, const SeqSpan& sp, int qb, float top, float sum, float* part_ml) const {
@@ -1080,16 +1088,183 @@ __global__ __launch_bounds__(256, 2) void paged_attn_wide_kernel(PagedRows b, At
   }
 }
 
+// float32, heads of 64 and 128: the same products on the 16 x 16 x 4 instructions, 16 columns to a workgroup, whose four wavefronts take
+// blocks of 16 keys in turn.  Every operand is loaded 16 bytes at a time straight into registers, because the contraction may run
+// in any order and the rows of a product may stand for any e:
+//   scores  lane (r16, g) holds K[r16][16 j + 4 g + i] and Q[r16][16 j + 4 g + i], i the step of four
+//   values  lane (r16, g) holds V[4 g + i][64 j + 4 r16 + x] and, from the scores, P[4 g + i]: x picks which quarter of the e a product has
+template <int HD>
+__global__ __launch_bounds__(256) void paged_attn_f32_kernel(PagedRows b, AttnRows a, int split_len, int col_tiles, float* part_o, float* part_ml) {
+  constexpr int KJ = HD / 16, VJ = HD / 64, STEP = 4 * 16;
+  __shared__ floatx4_t lds_o[4][VJ * 4][64];
+  __shared__ float lds_m[4][64], lds_l[4][64];
+  const int seq = blockIdx.z, hk = blockIdx.x, group = a.Hq / b.Hkv, split = blockIdx.y / col_tiles, col0 = blockIdx.y % col_tiles * 16;
+  const SeqSpan sp = seq_span(b, seq);
+  const Slice sl = slice_of(sp, split, split_len);
+  if (col0 >= sp.count * group || sl.key0 >= sl.key1) return;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, r16 = lane & 15, g = lane >> 4;
+  const int S = sp.n + sp.count, in_page = (1 << b.page_shift) - 1;
+  const size_t page_elems = (size_t)b.Hkv * HD << b.page_shift, head_elems = (size_t)hk * HD << b.page_shift;
+  const int32_t* table = b.table + (size_t)seq * b.table_width;
+  const float *kp = (const float*)a.k_pages + head_elems, *vp = (const float*)a.v_pages + head_elems;
+  const int col = col0 + r16, row = col / group, head = hk * group + col % group, row_here = row < sp.count ? row : sp.count - 1;
+  const uint64_t* mask = mask_of(a, sp, row);
+  struct __attribute__((packed, aligned(4))) Four {
+    floatx4_t v;
+  };
+
+  floatx4_t q[KJ], o[VJ][4];
+  const float* src = (const float*)a.q + (int64_t)(sp.row0 + row_here) * a.q_stride + (int64_t)head * HD + g * 4;
+#pragma unroll
+  for (int j = 0; j < KJ; ++j) q[j] = ((const Four*)(src + j * 16))->v;
+#pragma unroll
+  for (int j = 0; j < VJ; ++j)
+#pragma unroll
+    for (int x = 0; x < 4; ++x) o[j][x] = floatx4_t{0.f, 0.f, 0.f, 0.f};
+  float m = -INFINITY, l = 0.f;
+
+  auto page = [&](int slot) __attribute__((always_inline)) { return table[(slot < S ? slot : S - 1) >> b.page_shift]; };
+  floatx4_t kf[KJ], vf[4][VJ], kn[KJ], vn[4][VJ];
+  auto load = [&](floatx4_t (&k)[KJ], floatx4_t (&v)[4][VJ], int j0, int kid, int vid) __attribute__((always_inline)) {
+    const float* krow = kp + ((unsigned)kid < (unsigned)b.n_pages ? kid : 0) * page_elems + (size_t)((j0 + r16) & in_page) * HD + g * 4;
+    const float* vrow = vp + ((unsigned)vid < (unsigned)b.n_pages ? vid : 0) * page_elems + (size_t)((j0 + 4 * g) & in_page) * HD + r16 * 4;
+#pragma unroll
+    for (int j = 0; j < KJ; ++j) k[j] = ((const Four*)(krow + j * 16))->v;
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+#pragma unroll
+      for (int j = 0; j < VJ; ++j) v[i][j] = ((const Four*)(vrow + i * HD + j * 64))->v;
+  };
+  int j0 = sl.key0 + wave * 16;
+  if (j0 < sl.key1) {
+    int kid = page(j0 + r16), vid = page(j0 + 4 * g), kid_next = page(j0 + STEP + r16), vid_next = page(j0 + STEP + 4 * g);
+    load(kf, vf, j0, kid, vid);
+    for (; j0 < sl.key1; j0 += STEP) {
+      const int kid_after = page(j0 + 2 * STEP + r16), vid_after = page(j0 + 2 * STEP + 4 * g);
+      if (j0 + STEP < sl.key1) load(kn, vn, j0 + STEP, kid_next, vid_next);
+      // keys that are there; bit 0 is key j0
+      uint32_t there = (uint32_t)__ballot((unsigned)kid < (unsigned)b.n_pages && j0 + r16 < S) & 0xffffu;
+      const bool masked = there != 0xffffu || j0 + 16 > sp.n;
+      bool odd = false;
+      if (masked) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+#pragma unroll
+          for (int j = 0; j < VJ; ++j)
+#pragma unroll
+            for (int x = 0; x < 4; ++x) {
+              const bool here = there >> (4 * g + i) & 1, number = fabsf(vf[i][j][x]) < INFINITY;
+              odd |= here && !number;
+              vf[i][j][x] = here && number ? vf[i][j][x] : 0.f;
+            }
+      }
+      floatx4_t s = floatx4_t{0.f, 0.f, 0.f, 0.f}, s2 = s;               // two sums: one would wait for itself
+#pragma unroll
+      for (int j = 0; j < KJ; ++j)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          if (i & 1) s2 = __builtin_amdgcn_mfma_f32_16x16x4f32(kf[j][i], q[j][i], s2, 0, 0, 0);
+          else s = __builtin_amdgcn_mfma_f32_16x16x4f32(kf[j][i], q[j][i], s, 0, 0, 0);
+        }
+      s += s2;
+      uint32_t vis = 0;
+      if (masked) {
+        vis = (uint32_t)seen_bits(mask, sp, row, j0, there);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) s[i] = vis >> (4 * g + i) & 1 ? s[i] : -INFINITY;
+      }
+      const float best = max_over_groups(fmaxf(fmaxf(s[0], s[1]), fmaxf(s[2], s[3]))) * a.scale_log2, now = fmaxf(m, best);
+      const float ref = now == -INFINITY ? 0.f : now, keep = exp2f(m - ref);
+      m = now;
+      if (__any(keep != 1.0f)) {
+        l *= keep;
+#pragma unroll
+        for (int j = 0; j < VJ; ++j)
+#pragma unroll
+          for (int x = 0; x < 4; ++x) o[j][x] *= keep;
+      }
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        s[i] = exp2f(fmaf(s[i], a.scale_log2, -ref));
+        l += s[i];
+      }
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+#pragma unroll
+        for (int j = 0; j < VJ; ++j)
+#pragma unroll
+          for (int x = 0; x < 4; ++x) o[j][x] = __builtin_amdgcn_mfma_f32_16x16x4f32(vf[i][j][x], s[i], o[j][x], 0, 0, 0);
+      if (masked && __any(odd)) {                          // values that are no numbers, to the columns that see them: rare
+#pragma unroll 1
+        for (int key = 0; key < 16; ++key) {
+          if (!(there >> key & 1)) continue;
+          const int slot = j0 + key;
+          const float* v = vp + page(slot) * page_elems + (size_t)(slot & in_page) * HD + g * 16;
+#pragma unroll
+          for (int j = 0; j < VJ; ++j)
+#pragma unroll
+            for (int y = 0; y < 4; ++y)
+#pragma unroll
+              for (int x = 0; x < 4; ++x) {
+                const float z = v[j * 64 + 4 * y + x];
+                if (!(fabsf(z) < INFINITY) && (vis >> key & 1)) o[j][x][y] += z;
+              }
+        }
+      }
+#pragma unroll
+      for (int j = 0; j < KJ; ++j) kf[j] = kn[j];
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+#pragma unroll
+        for (int j = 0; j < VJ; ++j) vf[i][j] = vn[i][j];
+      kid = kid_next, vid = vid_next, kid_next = kid_after, vid_next = vid_after;
+    }
+  }
+
+  // ---- join the wavefronts
+  lds_m[wave][lane] = m;
+  lds_l[wave][lane] = sum_over_groups(l);
+#pragma unroll
+  for (int j = 0; j < VJ; ++j)
+#pragma unroll
+    for (int x = 0; x < 4; ++x) lds_o[wave][j * 4 + x][lane] = o[j][x];
+  __syncthreads();
+  float top = -INFINITY, f[4], sum = 0.f;
+#pragma unroll
+  for (int w = 0; w < 4; ++w) top = fmaxf(top, lds_m[w][lane]);
+  const float ref = top == -INFINITY ? 0.f : top;
+#pragma unroll
+  for (int w = 0; w < 4; ++w) {
+    f[w] = exp2f(lds_m[w][lane] - ref);
+    sum = fmaf(f[w], lds_l[w][lane], sum);
+  }
+  if (row >= sp.count) return;
+  const size_t at = (size_t)(sp.row0 + row) * a.Hq + head, rows = (size_t)b.rows * a.Hq;
+  // wavefront y: e = 64 j + 16 g + 4 y + x
+#pragma unroll
+  for (int j = 0; j < VJ; ++j) {
+    floatx4_t acc = floatx4_t{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int w = 0; w < 4; ++w)
+#pragma unroll
+      for (int x = 0; x < 4; ++x) acc[x] = fmaf(f[w], lds_o[w][j * 4 + x][lane][wave], acc[x]);
+    const int e0 = j * 64 + g * 16 + wave * 4;
+    if (sl.count > 1) *(floatx4_t*)(part_o + (split * rows + at) * HD + e0) = acc;
+    else store_four((float*)a.out + (int64_t)(sp.row0 + row) * a.out_stride + (int64_t)head * HD + e0, acc, sum);
+  }
+  if (sl.count > 1 && wave == 0 && g == 0) *(float2*)(part_ml + (split * rows + at) * 2) = make_float2(top, sum);
+}
+
 // out = sum_s 2^(m_s - m) O_s / sum_s 2^(m_s - m) l_s over the slices of a sequence, in a fixed order.  A workgroup per (row, head) and
 // up to PARTS groups of HD / 4 threads that take every PARTS-th slice, four elements a thread; their sums meet in LDS.
-template <int HD, int PARTS>
+template <typename T, int HD, int PARTS>
 __global__ __launch_bounds__(PARTS * (HD / 4)) void paged_attn_join_kernel(PagedRows b, AttnRows a, int split_len, const float* part_o,
                                                                           const float* part_ml) {
-  constexpr int T = HD / 4;
+  constexpr int QUADS = HD / 4;
   const SeqSpan sp = seq_span(b, blockIdx.z);
   const int count = slice_of(sp, 0, split_len).count, row = blockIdx.y, head = blockIdx.x;
   if (count <= 1 || row >= sp.count) return;
-  const int part = threadIdx.x / T, e = threadIdx.x % T * 4;
+  const int part = threadIdx.x / QUADS, e = threadIdx.x % QUADS * 4;
   const size_t rows = (size_t)b.rows * a.Hq, mine = (size_t)(sp.row0 + row) * a.Hq + head;
   __shared__ float lds_o[PARTS][HD];
   __shared__ float2 lds_ml[PARTS];
@@ -1136,9 +1311,7 @@ __global__ __launch_bounds__(PARTS * (HD / 4)) void paged_attn_join_kernel(Paged
       for (int c = 0; c < 4; ++c) acc[c] = fmaf(f, x[c], acc[c]);
     }
   }
-  const float inv = sum == 0.f ? 0.f : 1.0f / sum;
-  ((Loose8*)((bf16_t*)a.out + (int64_t)(sp.row0 + row) * a.out_stride + (int64_t)head * HD + e))->v =
-      sum == 0.f ? make_uint2(0, 0) : pack4_bf16(acc[0] * inv, acc[1] * inv, acc[2] * inv, acc[3] * inv);
+  store_four((T*)a.out + (int64_t)(sp.row0 + row) * a.out_stride + (int64_t)head * HD + e, acc, sum);
 }
 
 // The same for shared-out work.  A workgroup per part; those of an item share the item's elements out among them, four elements to a unit, and where that leaves fewer units than threads, the threads share the parts.
@@ -1212,21 +1385,22 @@ __global__ __launch_bounds__(256) void paged_attn_share_join_kernel(PagedRows b,
 namespace {
 // How a call runs: from its bounds alone, so that a captured call fits whatever its tables say later
 struct AttnPlan {
-  bool simple, few;
-  int blocks;                    // few: column blocks of 16
+  bool simple, few, f32;
+  int blocks;                    // few: column blocks of 16 (f32: a workgroup each)
   int split_len, splits;         // few
   int cols, workgroups, least;   // shared-out work: columns of an item, workgroups (0: one to an item), the least tiles of one
 };
 AttnPlan attn_plan(int dtype, const PagedRows& b, int Hq) {
   AttnPlan p{};
   const int cols = b.max_rows * (Hq / b.Hkv), S = b.max_len + b.max_rows;
-  p.simple = dtype == 0 || (b.hd != 64 && b.hd != 128);
+  p.simple = b.hd != 64 && b.hd != 128;
   p.split_len = S, p.splits = 1;
   if (p.simple) return p;
-  p.few = cols <= 32;
+  p.f32 = dtype == 0;
+  p.few = p.f32 || cols <= 32;
   if (p.few) {
-    p.blocks = cols <= 16 ? 1 : 2;
-    const int64_t groups = (int64_t)b.seqs * b.Hkv, want = 1024;
+    p.blocks = p.f32 ? (cols + 15) / 16 : cols <= 16 ? 1 : 2;
+    const int64_t groups = (int64_t)b.seqs * b.Hkv * (p.f32 ? p.blocks : 1), want = 1024;
     const int least = 256;
     int64_t splits = (want + groups - 1) / groups;
     if (splits > S / least) splits = S / least;
@@ -1255,12 +1429,17 @@ size_t part_columns(const AttnPlan& p, const PagedRows& b, int Hq) {        // c
 template <int HD>
 hipError_t launch_attn_hd(const AttnPlan& p, const PagedRows& b, const AttnRows& a, float* part_o, float* part_ml, PartNote* notes, hipStream_t s) {
   if (p.few) {
-    auto f = p.blocks == 1 ? paged_attn_few_kernel<HD, 1> : paged_attn_few_kernel<HD, 2>;
-    hipLaunchKernelGGL(f, dim3(b.Hkv, p.splits, b.seqs), dim3(256), 0, s, b, a, p.split_len, part_o, part_ml);
+    if (p.f32) {
+      hipLaunchKernelGGL(paged_attn_f32_kernel<HD>, dim3(b.Hkv, p.splits * p.blocks, b.seqs), dim3(256), 0, s, b, a, p.split_len, p.blocks, part_o, part_ml);
+    } else {
+      auto f = p.blocks == 1 ? paged_attn_few_kernel<HD, 1> : paged_attn_few_kernel<HD, 2>;
+      hipLaunchKernelGGL(f, dim3(b.Hkv, p.splits, b.seqs), dim3(256), 0, s, b, a, p.split_len, part_o, part_ml);
+    }
     if (p.splits > 1) {
-      const dim3 rows(a.Hq, b.max_rows, b.seqs);
-      if (p.splits > 4) hipLaunchKernelGGL((paged_attn_join_kernel<HD, 8>), rows, dim3(8 * HD / 4), 0, s, b, a, p.split_len, part_o, part_ml);
-      else hipLaunchKernelGGL((paged_attn_join_kernel<HD, 1>), rows, dim3(HD / 4), 0, s, b, a, p.split_len, part_o, part_ml);
+      const bool many = p.splits > 4;
+      auto j = p.f32 ? (many ? paged_attn_join_kernel<float, HD, 16> : paged_attn_join_kernel<float, HD, 1>)
+                     : (many ? paged_attn_join_kernel<bf16_t, HD, 16> : paged_attn_join_kernel<bf16_t, HD, 1>);
+      hipLaunchKernelGGL(j, dim3(a.Hq, b.max_rows, b.seqs), dim3((many ? 16 : 1) * HD / 4), 0, s, b, a, p.split_len, part_o, part_ml);
     }
     return hipGetLastError();
   }
