@@ -1820,7 +1820,8 @@ int check_paged(const ht_paged_batch* b, PagedRows* out) {
   return HT_OK;
 }
 int check_heads(const ht_paged_batch* b, int32_t Hq) {
-  if (Hq < 1 || Hq > 65535 || Hq % b->n_kv_heads) return fail(HT_EINVAL, "%d query heads for %d key/value heads", Hq, b->n_kv_heads);
+  if (Hq < 1 || Hq > 65535 || Hq % b->n_kv_heads || Hq / b->n_kv_heads > 256)
+    return fail(HT_EINVAL, "%d query heads for %d key/value heads", Hq, b->n_kv_heads);
   return HT_OK;
 }
 }  // namespace

@@ -39,7 +39,7 @@ hipError_t launch_tree_tables(const PagedRows& b, const int32_t* parent, int32_t
 }
 
 // ------------------------------------------------------------------------------------------------ append
-// A wavefront per head of a row: lane l holds the pairs l, l + 64 of the rotated part and what it passes through.
+// Any head width: a wavefront per head of a row, lane l holds the pairs l, l + 64 of the rotated part and what it passes through.
 template <typename T>
 __global__ __launch_bounds__(256) void paged_append_kernel(PagedRows b, AppendRows a) {
   const SeqSpan sp = seq_span(b, blockIdx.z);
@@ -113,10 +113,116 @@ __global__ __launch_bounds__(256) void paged_append_kernel(PagedRows b, AppendRo
     Conv<T>::store(dst + hi[t], w);
   }
 }
+// Heads of whole 16-byte pieces whose number is a power of two: a row's heads P at a time for every hd / VEC threads, all of them
+// requested before the factors are worked out (by as many threads as there are pairs, once for all heads of the workgroup).  Partners of a
+// pair lie in one thread, or rot / 2 entries, whole pieces, apart in the same wavefront.  Bound by what the rows stream at once there are
+// many; for few by the chain row start, length, depth, factors.
+template <typename T, int P>
+__global__ __launch_bounds__(256) void paged_append_vec_kernel(PagedRows b, AppendRows a) {
+  constexpr int VEC = 16 / sizeof(T);
+  struct __attribute__((packed, aligned(sizeof(T)))) Piece {
+    T v[VEC];
+  };
+  const SeqSpan sp = seq_span(b, blockIdx.z);
+  const int i = blockIdx.y;
+  if (i >= sp.count) return;
+  __shared__ __attribute__((aligned(16))) float2 factors[128];
+  const int tid = threadIdx.x, row = sp.row0 + i, half = a.rot / 2, slot = sp.n + i;
+  const int per_head = b.hd / VEC, at_once = 256 / per_head, p = tid % per_head, heads = a.Hq + 2 * b.Hkv;
+  const int h0 = blockIdx.x * P * at_once + tid / per_head;
+  // kind 0: query, 1: key, 2: value, 3: none
+  auto kind_of = [&](int h) { return h >= heads ? 3 : h < a.Hq ? (a.q ? 0 : 3) : !a.k ? 3 : h < a.Hq + b.Hkv ? 1 : 2; };
+  auto head_of = [&](int h, int kind) { return kind == 0 ? h : h - a.Hq - (kind == 2 ? b.Hkv : 0); };
+  Piece x[P];
+#pragma unroll
+  for (int k = 0; k < P; ++k) {
+    const int h = h0 + k * at_once, kind = kind_of(h);
+    if (kind == 3) continue;
+    const T* src = kind == 0 ? (const T*)a.q + row * a.q_stride : kind == 1 ? (const T*)a.k + row * a.k_stride : (const T*)a.v + row * a.v_stride;
+    x[k] = *(const Piece*)(src + (size_t)head_of(h, kind) * b.hd + p * VEC);
+  }
+  const int page = a.k ? page_of(b, blockIdx.z, slot) : -1;
+  const int pos = sp.n + (a.depth ? a.depth[row] : i);
+  if (tid < half) {
+    const float2 f = rope_factor(pos, a.inv_freq ? freq_turns(a.inv_freq[tid]) : rope_turns(tid, a.step));
+    factors[tid] = make_float2(f.x * a.amplitude, f.y * a.amplitude);
+  }
+  __syncthreads();
+  const int half_pieces = half / VEC;                      // pairs apart: pieces between partners
+  const bool turns = a.interleaved ? p * VEC < a.rot : p < 2 * half_pieces, upper = p >= half_pieces;
+  const int partner = (tid & 63) + (!turns || a.interleaved ? 0 : upper ? -half_pieces : half_pieces);
+#pragma unroll
+  for (int k = 0; k < P; ++k) {
+    const int h = h0 + k * at_once, kind = kind_of(h);
+    float y[VEC];
+#pragma unroll
+    for (int c = 0; c < VEC; ++c) y[c] = kind == 3 ? 0.f : Conv<T>::load(&x[k].v[c]);
+    const T* gain = kind == 0 ? (const T*)a.q_gain : kind == 1 ? (const T*)a.k_gain : nullptr;
+    if (a.q_gain || a.k_gain) {                            // (the same for the wavefront: the exchange needs all of it)
+      float ss = 0.f;
+#pragma unroll
+      for (int c = 0; c < VEC; ++c) ss = fmaf(y[c], y[c], ss);
+      for (int o = per_head / 2; o; o >>= 1) ss += __shfl_xor(ss, o, 64);
+      if (gain) {
+        const float r = 1.0f / sqrtf(ss / (float)b.hd + a.eps);
+        const Piece g = *(const Piece*)(gain + p * VEC);
+#pragma unroll
+        for (int c = 0; c < VEC; ++c) y[c] = y[c] * r * Conv<T>::load(&g.v[c]);
+      }
+    }
+    if (a.rot && !a.interleaved) {
+      float z[VEC];
+#pragma unroll
+      for (int c = 0; c < VEC; ++c) z[c] = __shfl(y[c], partner, 64);
+      if (kind < 2 && turns) {
+#pragma unroll
+        for (int c = 0; c < VEC; ++c) {
+          const float2 f = factors[(upper ? p - half_pieces : p) * VEC + c];
+          y[c] = upper ? rope_high(z[c], y[c], f) : rope_low(y[c], z[c], f);
+        }
+      }
+    } else if (kind < 2 && turns) {
+#pragma unroll
+      for (int c = 0; c < VEC; c += 2) {
+        if (p * VEC + c >= a.rot) break;
+        const float2 f = factors[(p * VEC + c) / 2];
+        const float lo = rope_low(y[c], y[c + 1], f);
+        y[c + 1] = rope_high(y[c], y[c + 1], f);
+        y[c] = lo;
+      }
+    }
+    if (kind == 3 || (kind && page < 0)) continue;
+    Piece out;
+    if (kind == 2) out = x[k];
+    else
+#pragma unroll
+      for (int c = 0; c < VEC; ++c) Conv<T>::store(&out.v[c], y[c]);
+    T* dst;
+    if (kind == 0) dst = (T*)a.q_out + row * a.q_out_stride + (size_t)h * b.hd;
+    else
+      dst = (T*)(kind == 1 ? a.k_pages : a.v_pages) +
+            ((((size_t)page * b.Hkv + head_of(h, kind)) << b.page_shift) + (slot & ((1 << b.page_shift) - 1))) * b.hd;
+    *(Piece*)(dst + p * VEC) = out;
+  }
+}
+template <typename T> void launch_append_of(const PagedRows& b, const AppendRows& a, hipStream_t s) {
+  constexpr int VEC = 16 / sizeof(T);
+  const int heads = a.Hq + 2 * b.Hkv, pieces = b.hd / VEC;
+  // pieces of a head: whole, a power of two, within a wavefront; partners whole pieces apart
+  if (b.hd % VEC || pieces > 64 || (pieces & (pieces - 1)) || (!a.interleaved && (a.rot / 2) % VEC)) {
+    hipLaunchKernelGGL(paged_append_kernel<T>, dim3((heads + 3) / 4, b.max_rows, b.seqs), dim3(256), 0, s, b, a);
+    return;
+  }
+  // heads four at a time for a thread once there are rows for every unit several times over, one where latency counts
+  const int at_once = 256 / pieces;
+  const int64_t rows = (int64_t)b.max_rows * b.seqs;
+  const int P = rows >= 512 ? 4 : rows >= 128 ? 2 : 1;
+  auto f = P == 4 ? paged_append_vec_kernel<T, 4> : P == 2 ? paged_append_vec_kernel<T, 2> : paged_append_vec_kernel<T, 1>;
+  hipLaunchKernelGGL(f, dim3((heads + P * at_once - 1) / (P * at_once), b.max_rows, b.seqs), dim3(256), 0, s, b, a);
+}
 hipError_t launch_paged_append(int dtype, const PagedRows& b, const AppendRows& a, hipStream_t s) {
-  const dim3 grid((a.Hq + 2 * b.Hkv + 3) / 4, b.max_rows, b.seqs);
-  if (dtype == 0) hipLaunchKernelGGL(paged_append_kernel<float>, grid, dim3(256), 0, s, b, a);
-  else hipLaunchKernelGGL(paged_append_kernel<bf16_t>, grid, dim3(256), 0, s, b, a);
+  if (dtype == 0) launch_append_of<float>(b, a, s);
+  else launch_append_of<bf16_t>(b, a, s);
   return hipGetLastError();
 }
 
