@@ -12,7 +12,8 @@
 // pass unrolled over them, the passes' own needs went to scratch memory.)  A prefix of the order ends at one element (value, index),
 // so a filter is a search for that element, not a sort of the row:
 //   top-k    the k-th largest of the 1024 threads' maxima is no larger than the k-th largest value, so the elements from there on hold
-//            the first k; they are a few more than k, are listed and sorted, and top-p, min-p and the draw work on the list.
+//            the first k; they are a few more than k, are listed and sorted, and top-p, min-p and the draw work on the list.  A larger
+//            k up to 1024 is searched for as below by counts, and what it kept is listed then.
 //   top-p alone, or a k that makes the list too long: a histogram of masses (or counts) over 2048 equal steps of the value finds the
 //            step that holds the end, whose elements are listed and ranked; a step that holds too many becomes the next
 //            histogram's range (a value far below the others, as masks leave, costs such a round).  Its masses are counted in whole
@@ -276,8 +277,8 @@ __global__ __launch_bounds__(kThreads) void sample_rows_kernel(SampleRows a) {
   int cut_i = -1;
   auto kept = [&](float x, int i) __attribute__((always_inline)) { return (x > cut_x) | ((x == cut_x) & (i <= cut_i)); };
 
-  // `loose` (n of them) into `keys`, ascending, with their e
-  auto sort_list = [&](int n) __attribute__((always_inline)) {
+  // `loose` (n different ones) into `keys`, ascending
+  auto sort_keys = [&](int n) __attribute__((always_inline)) {
     if (n <= kShort) {
       // four threads count a quarter of the list each for an element
       const int who = tid >> 2, part = tid & 3, whole_n = (n + 31) & ~31;
@@ -291,10 +292,7 @@ __global__ __launch_bounds__(kThreads) void sample_rows_kernel(SampleRows a) {
       }
       rank += __shfl_xor(rank, 1, 64);
       rank += __shfl_xor(rank, 2, 64);
-      if (who < n && part == 0) {
-        keys[rank] = key;
-        shares[rank] = energy(of_ordered(~(uint32_t)(key >> 32)));
-      }
+      if (who < n && part == 0) keys[rank] = key;
     } else {
       // bitonic, strides below 64 inside a wavefront
       int size = 512;
@@ -317,7 +315,6 @@ __global__ __launch_bounds__(kThreads) void sample_rows_kernel(SampleRows a) {
         }
       __syncthreads();
       if (tid < size) keys[tid] = key;
-      if (tid < n) shares[tid] = energy(of_ordered(~(uint32_t)(key >> 32)));
     }
     __syncthreads();
   };
@@ -417,7 +414,7 @@ __global__ __launch_bounds__(kThreads) void sample_rows_kernel(SampleRows a) {
         lo = of_ordered(found.lo), hi = of_ordered(found.hi);
         continue;
       }
-      sort_list(n);
+      sort_keys(n);
       const unsigned long long w = tid < n ? weight(of_ordered(~(uint32_t)(keys[tid] >> 32))) : 0, up_to = above + block_run(w, 0ull);
       if (up_to - w < need && up_to >= need) found.index = tid;
       __syncthreads();
@@ -448,8 +445,9 @@ __global__ __launch_bounds__(kThreads) void sample_rows_kernel(SampleRows a) {
     const float v = block_fold(bin >= 0 && best > -INFINITY && bin_of(best) <= bin ? best : top, top, smaller);
     return bin < 0 ? -INFINITY : v;
   };
-  // The elements from `from` on, sorted: their number, or more than kList if they are too many to list
+  // The kept elements from `from` on, sorted, with their e: their number, or more than kList if they are too many to list
   auto list_from = [&](float from) __attribute__((always_inline)) -> int {
+    __syncthreads();
     if (tid == 0) found.listed = 0;
     __syncthreads();
     if (best >= from)
@@ -460,7 +458,7 @@ __global__ __launch_bounds__(kThreads) void sample_rows_kernel(SampleRows a) {
         if (!some) return;
 #pragma unroll
         for (int c = 0; c < VEC; ++c)
-          if (x[c] >= from && x[c] > -INFINITY) {
+          if (x[c] >= from && kept(x[c], i0 + c)) {
             const int at = atomicAdd(&found.listed, 1);
             if (at < kList) loose[at] = key_of(x[c], i0 + c);
           }
@@ -468,7 +466,9 @@ __global__ __launch_bounds__(kThreads) void sample_rows_kernel(SampleRows a) {
     __syncthreads();
     const int n = found.listed;
     if (n > kList) return n;
-    sort_list(n);
+    sort_keys(n);
+    if (tid < n) shares[tid] = energy(of_ordered(~(uint32_t)(keys[tid] >> 32)));
+    __syncthreads();
     return n;
   };
 
@@ -490,6 +490,7 @@ __global__ __launch_bounds__(kThreads) void sample_rows_kernel(SampleRows a) {
     } else {
       low = block_fold(low, INFINITY, smaller);
       search([](float) __attribute__((always_inline)) -> unsigned long long { return 1; }, (unsigned long long)k, -1.0, fmaxf(from, low), top);
+      if (k <= kList && cut_x > -INFINITY) kept_list = list_from(cut_x);         // (k of them)
     }
   }
   if (cut_p && kept_list) {
@@ -538,7 +539,23 @@ __global__ __launch_bounds__(kThreads) void sample_rows_kernel(SampleRows a) {
     if (a.logprob) a.logprob[row] = (float)log(mine / total);
     return;
   }
-  if (kept_list) cut_at(kept_list - 1);
+  if (kept_list) {
+    // the same with the list sorted by index
+    if (tid < kept_list) loose[tid] = (unsigned long long)(uint32_t)keys[tid] << 32 | (uint32_t)tid;
+    __syncthreads();
+    sort_keys(kept_list);
+    const double e = tid < kept_list ? shares[(uint32_t)keys[tid]] : 0.0, run = block_run(e, 0.0);
+    if (tid == kThreads - 1) found.total = run;
+    __syncthreads();
+    const double total = found.total, target = u * total;
+    const int past = block_fold(e > kNothing && run > target ? tid : INT32_MAX, INT32_MAX, smaller);
+    const int last = block_fold(e > kNothing ? tid : -1, -1, larger);
+    if (tid == (past < INT32_MAX ? past : last)) {
+      a.tokens[row] = (int)(keys[tid] >> 32);
+      if (a.logprob) a.logprob[row] = (float)log(e / total);
+    }
+    return;
+  }
   // min-p: what lies well below its border by value is not worth an exponential
   if (least > 0.0) {
     const float near = nextafterf((float)((double)top + (double)temp * (log(least) - 1e-3)), -INFINITY);
