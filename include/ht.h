@@ -366,7 +366,8 @@ typedef struct {
 
 /* Queries and keys through `turn` at position len[s] + depth (depth NULL: the row's number in its sequence), keys and values into
  * their slots.  q [rows, Hq, head_dim], k, v [rows, n_kv_heads, head_dim], consecutive rows *_stride elements apart (the parts of a
- * fused projection need no copy); q_out may be q.  q NULL: keys and values only; k and v NULL: queries only. */
+ * fused projection need no copy); q_out may be q, and overlaps no input otherwise.  len[s] + depth has to fit in 32 bits.  q NULL: keys
+ * and values only; k and v NULL: queries only.  Hq: a multiple of n_kv_heads, at most 256 times as many (HT_EINVAL). */
 int ht_paged_append(const ht_paged_batch *batch, const ht_head_turn *turn, int32_t Hq, const void *q, int64_t q_stride,
                     const void *k, int64_t k_stride, const void *v, int64_t v_stride, const int32_t *depth, void *q_out,
                     int64_t q_out_stride, void *k_pages, void *v_pages, void *stream);
@@ -375,7 +376,8 @@ int ht_paged_append(const ht_paged_batch *batch, const ht_head_turn *turn, int32
  * `anc` name (NULL: itself and the rows before it: a prompt's chunk, or one token), whose keys and values ht_paged_append has
  * stored.  out [rows, Hq, head_dim] = softmax(scale q.k) v; scale 0 means 1 / sqrt(head_dim).  Keys and values that a row does not see do
  * not matter, whatever they hold; a row that sees nothing is 0.  Softmax and sums in float32.  Query heads h / (Hq / n_kv_heads)
- * share a key/value head.  scratch: device, 256-byte aligned, >= ht_paged_attention_scratch_bytes (0 for a bad batch), of this call alone
+ * share a key/value head, up to 256 of them (HT_EINVAL).  out may be q, and overlaps nothing else.  k_pages and v_pages: 16-byte
+ * aligned (HT_EINVAL).  scratch: device, 256-byte aligned, >= ht_paged_attention_scratch_bytes (0 for a bad batch), of this call alone
  * while it runs. */
 size_t ht_paged_attention_scratch_bytes(const ht_paged_batch *batch, int32_t Hq);
 int ht_paged_attention(const ht_paged_batch *batch, int32_t Hq, const void *q, int64_t q_stride, const void *k_pages,

@@ -296,6 +296,8 @@ class PagedBatch:
             raise _bad("the pages are not on a GPU")
         if k_pages.dtype not in _DTYPES or k_pages.dim() not in (4, 5) or page_table.dim() != 2:
             raise _bad("pages are [n_pages, n_kv_heads, page_rows, head_dim] of float32 or bfloat16, the page table [seqs, width]")
+        if not all(0 <= n < 1 << 31 for n in (rows, max_rows, max_len, *k_pages.shape[-4:], *page_table.shape)):
+            raise _bad("a number outside 0 .. 2^31 - 1")        # (the C structure would take it modulo 2^32)
         self.device, self.dtype, self.pool = k_pages.device, k_pages.dtype, tuple(k_pages.shape[-4:])
         self.seqs, self.rows = page_table.shape[0], rows
         c = self.c = ht_paged_batch()
@@ -395,6 +397,8 @@ def ht_sample_rows(logits, u, temperature=None, top_k=None, top_p=None, min_p=No
     if dev.type != "cuda" or logits.dim() != 2 or logits.dtype not in _DTYPES or (logits.shape[1] > 1 and logits.stride(1) != 1):
         raise _bad("logits are rows of float32 or bfloat16 on a GPU")
     rows, V = logits.shape
+    if rows >> 31 or V >> 31:
+        raise _bad(f"logits of {rows} x {V}")
     if u is None:
         raise _bad("u is None")
     f, i = torch.float32, torch.int32

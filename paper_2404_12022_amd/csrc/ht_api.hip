@@ -1878,6 +1878,7 @@ int ht_paged_attention(const ht_paged_batch* batch, int32_t Hq, const void* q, i
   if (q_stride < (int64_t)Hq * b.hd || out_stride < (int64_t)Hq * b.hd) return fail(HT_EINVAL, "a row stride is shorter than the row");
   if (scratch_bytes < ht_paged_attention_scratch_bytes(batch, Hq)) return fail(HT_EINVAL, "scratch too small");
   if ((uintptr_t)scratch % 256) return fail(HT_EINVAL, "scratch must be 256-byte aligned");
+  if (((uintptr_t)k_pages | (uintptr_t)v_pages) % 16) return fail(HT_EINVAL, "k_pages and v_pages must be 16-byte aligned");
   const double s = scale > 0.f ? (double)scale : 1.0 / sqrt((double)b.hd);
   AttnRows a{q, k_pages, v_pages, q_stride, out_stride, anc, out, (float)(s * 1.4426950408889634), Hq};
   HT_HIP(launch_paged_attn(batch->dtype, b, a, scratch, (hipStream_t)stream));

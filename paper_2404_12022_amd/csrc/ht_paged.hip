@@ -290,7 +290,7 @@ __global__ __launch_bounds__(256) void paged_accept_kernel(PagedRows b, AcceptRo
 }
 hipError_t launch_paged_accept(int dtype, const PagedRows& b, const AcceptRows& a, int layers, hipStream_t s) {
   const int elem = dtype == 0 ? 4 : 2;
-  const bool wide = b.hd * elem % 16 == 0 && !(((uintptr_t)a.k_pages | (uintptr_t)a.v_pages) & 15);
+  const bool wide = b.hd * elem % 16 == 0 && !(((uintptr_t)a.k_pages | (uintptr_t)a.v_pages | a.layer_elems * elem) & 15);
   const int unit = wide ? 16 / elem : 1, units = b.Hkv * b.hd / unit;
   const dim3 grid((2 * units + 255) / 256, layers, b.seqs);
   if (wide) hipLaunchKernelGGL(paged_accept_kernel<uint4>, grid, dim3(256), 0, s, b, a, unit, units);

@@ -927,7 +927,7 @@ template <int HD> struct WideColumns {
 // 64 x 16 bytes from `base` + off (a lane's own) to 1 KiB of LDS at `to`.  Written out because a read of LDS behind such a load, wherever it
 // goes, makes the compiler wait for it; this way the waits are those of wait_then_barrier.  The load writes no register.
 __device__ __forceinline__ void load_to_lds(const char* base, uint32_t off, uint32_t to) {
-  asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1" ::"v"(off), "s"(base), "s"(to) : "memory");
+  asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1" ::"v"(off), "s"(base), "s"(to) : "memory", "m0");
 }
 __device__ __forceinline__ void wait_then_barrier() { asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
 __device__ __forceinline__ uint32_t lds_address(const void* p) { return (uint32_t)(uintptr_t)(__attribute__((address_space(3))) const void*)p; }

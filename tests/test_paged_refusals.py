@@ -90,6 +90,15 @@ def test_attention_refuses():
         assert call(**bad) == B.HT_EINVAL, bad
 
 
+def test_pages_of_attention_lie_on_16_bytes_and_groups_end_at_256():
+    b = batch(n_kv_heads=1)
+    need = B.lib.ht_paged_attention_scratch_bytes(C.byref(b), 256)
+    assert need > 0 and B.lib.ht_paged_attention_scratch_bytes(C.byref(b), 257) == 0
+    call = lambda Hq, kp, vp: code("ht_paged_attention", C.byref(b), Hq, P, FAR, kp, vp, None, 0.0, P, FAR, P, FAR, None)  # noqa: E731
+    assert call(257, P, P) == call(4, P + 8, P) == call(4, P, P + 2) == B.HT_EINVAL
+    assert code("ht_paged_append", C.byref(b), C.byref(turn()), 257, P, FAR, P, FAR, P, FAR, None, P, FAR, P, P, None) == B.HT_EINVAL
+
+
 def test_sampling_refuses():
     ok = dict(z=P, stride=100, dtype=B.HT_F32, rows=3, V=100, u=P, tok=P)
 
