@@ -213,11 +213,12 @@ template <typename T> void launch_append_of(const PagedRows& b, const AppendRows
     hipLaunchKernelGGL(paged_append_kernel<T>, dim3((heads + 3) / 4, b.max_rows, b.seqs), dim3(256), 0, s, b, a);
     return;
   }
-  // heads four at a time for a thread once there are rows for every unit several times over, one where latency counts
+  // two heads to a thread once the rows are many (64 sequences of 64 rows, 32 heads of 128: 33 us, with one 37, with four 40), one
+  // before (16 of 64: 12.3 us, with two 12.7, four 15.7; one row: 3.9, 4.7, 6.3)
   const int at_once = 256 / pieces;
   const int64_t rows = (int64_t)b.max_rows * b.seqs;
-  const int P = rows >= 512 ? 4 : rows >= 128 ? 2 : 1;
-  auto f = P == 4 ? paged_append_vec_kernel<T, 4> : P == 2 ? paged_append_vec_kernel<T, 2> : paged_append_vec_kernel<T, 1>;
+  const int P = rows >= 2048 ? 2 : 1;
+  auto f = P == 2 ? paged_append_vec_kernel<T, 2> : paged_append_vec_kernel<T, 1>;
   hipLaunchKernelGGL(f, dim3((heads + P * at_once - 1) / (P * at_once), b.max_rows, b.seqs), dim3(256), 0, s, b, a);
 }
 hipError_t launch_paged_append(int dtype, const PagedRows& b, const AppendRows& a, hipStream_t s) {

@@ -432,20 +432,10 @@ template <int HD, int QB> struct Columns {
     }
   }
 
-  // Column (qb, r16): o and the sum over its four lanes, to `out` or to the split's partial results
-  __device__ __forceinline__ void finish(const AttnRows& a, const SeqSpan& sp, int qb, const floatx4_t& acc, int eb, float sum, int g,
-                                         float* part_o) const {
-    if (row[qb] >= sp.count) return;
-    const int64_t at = (int64_t)(sp.row0 + row[qb]);
-    const int e0 = eb * 16 + g * 4;
-    if (part_o) {
-      *(float4*)(part_o + (at * a.Hq + head[qb]) * HD + e0) = make_float4(acc[0], acc[1], acc[2], acc[3]);
-    } else {
-      store_four((bf16_t*)a.out + at * a.out_stride + (int64_t)head[qb] * HD + e0, acc, sum);
-    }
-  }
-  __device__ __forceinline__ void finish_sum(const AttnRows& a, const SeqSpan& sp, int qb, float top, float sum, float* part_ml) const {
-    if (row[qb] < sp.count) *(float2*)(part_ml + ((int64_t)(sp.row0 + row[qb]) * a.Hq + head[qb]) * 2) = make_float2(top, sum);
+  // Column (qb, r16): o over its sum
+  __device__ __forceinline__ void finish(const AttnRows& a, const SeqSpan& sp, int qb, const floatx4_t& acc, int eb, float sum, int g) const {
+    if (row[qb] < sp.count)
+      store_four((bf16_t*)a.out + (int64_t)(sp.row0 + row[qb]) * a.out_stride + (int64_t)head[qb] * HD + eb * 16 + g * 4, acc, sum);
   }
 };
 
@@ -459,101 +449,128 @@ __device__ __forceinline__ Slice slice_of(const SeqSpan& sp, int split, int spli
   return Slice{k0, k0 + split_len < S ? k0 + split_len : S, count};
 }
 
-// Shared-out work of the kernels for many columns.  An item is a (head, sequence, column tile); a long one is cut into parts, a workgroup
-// each, none of more than T tiles with kItemTiles for what starting and ending costs, T the smallest with which all parts fit the
+// Shared-out work of the bf16 kernels.  An item is a (head, sequence, column tile); a long one is cut into parts, a workgroup each, none
+// of more than T tiles of 64 keys with `ITEM` for what starting and ending costs, T the smallest with which all parts fit the
 // grid: lengths may be as ragged as they like.  The parts of an item leave partial results, which a second kernel joins.  Every
-// wavefront works this out for itself.  Workgroups of one XCD (numbers that are equal modulo 8) have consecutive parts, heads
-// outermost: column tiles of the same keys meet in one L2.
+// wavefront works this out for itself.
 constexpr int kShareSeqs = 256;              // sequences that a wavefront can add up
-constexpr int kItemTiles = 3;                // 5 to 6 us of a workgroup; a tile 1.9
+constexpr int kFewItem = 2, kManyItem = 3;    // tiles that starting and ending a part costs: TODO
 struct Part {
   int seq, hk, col_tile, key0, key1;
   int parts, part, place;                    // of the item: how many, which, and where in the row of parts this one stands
+  SeqSpan sp;
 };
 // What a workgroup leaves for the join; parts 0: nothing, 1: a whole item
 struct PartNote {
-  int32_t seq, hk, col_tile, part, parts, pad[3];
+  int32_t row0, count, hk, col_tile, part, parts, pad[2];
 };
-__device__ __forceinline__ int wave_total(int v) {
-#pragma unroll
-  for (int o = 32; o; o >>= 1) v += __shfl_xor(v, o, 64);
-  return __builtin_amdgcn_readfirstlane(v);
+// Running sums over a wavefront, by moves that need no LDS; lane 63 has them all
+__device__ __forceinline__ int wave_sums(int v) {
+  v += __builtin_amdgcn_update_dpp(0, v, 0x111, 0xf, 0xf, false);        // from the lanes 1, 2, 4, 8 before in the row of 16
+  v += __builtin_amdgcn_update_dpp(0, v, 0x112, 0xf, 0xf, false);
+  v += __builtin_amdgcn_update_dpp(0, v, 0x114, 0xf, 0xf, false);
+  v += __builtin_amdgcn_update_dpp(0, v, 0x118, 0xf, 0xf, false);
+  v += __builtin_amdgcn_update_dpp(0, v, 0x142, 0xa, 0xf, false);        // from the last lane of the row before
+  v += __builtin_amdgcn_update_dpp(0, v, 0x143, 0xc, 0xf, false);        // from lane 31
+  return v;
 }
-// False: nothing for this workgroup
-__device__ __forceinline__ bool part_of_workgroup(const PagedRows& b, int group, int cols, int least, Part& out) {
-  constexpr int PER = kShareSeqs / 64;
+__device__ __forceinline__ int wave_total(int v) { return __builtin_amdgcn_readlane(wave_sums(v), 63); }
+__device__ __forceinline__ int wave_largest(int v) {                      // of numbers >= 0
+  auto step = [&](int other) { v = other > v ? other : v; };
+  step(__builtin_amdgcn_update_dpp(0, v, 0x111, 0xf, 0xf, false));
+  step(__builtin_amdgcn_update_dpp(0, v, 0x112, 0xf, 0xf, false));
+  step(__builtin_amdgcn_update_dpp(0, v, 0x114, 0xf, 0xf, false));
+  step(__builtin_amdgcn_update_dpp(0, v, 0x118, 0xf, 0xf, false));
+  step(__builtin_amdgcn_update_dpp(0, v, 0x142, 0xa, 0xf, false));
+  step(__builtin_amdgcn_update_dpp(0, v, 0x143, 0xc, 0xf, false));
+  return __builtin_amdgcn_readlane(v, 63);
+}
+// The place of a workgroup in the row of parts.  Where several column tiles read the same keys, the workgroups of one XCD (numbers that
+// are equal modulo 8) have consecutive parts, heads outermost, so that they meet in one L2.
+template <bool TILES> __device__ __forceinline__ int place_of_workgroup() {
+  const int per = gridDim.x / 8;
+  return !TILES || gridDim.x % 8 ? blockIdx.x : blockIdx.x % 8 * per + blockIdx.x / 8;
+}
+// Which part this workgroup has of a batch of up to 64 PER sequences; false: none
+template <int COLS, int ITEM, int PER>
+__device__ __forceinline__ bool share_out(const PagedRows& b, int group, int least, Part& out) {
   const int lane = threadIdx.x & 63;
-  if (!least) {                                            // an item to a workgroup
-    const SeqSpan sp = seq_span(b, blockIdx.z);
-    out = Part{(int)blockIdx.z, (int)blockIdx.x, (int)blockIdx.y, 0, sp.n + sp.count, 1, 0, 0};
-    return (int)blockIdx.y * cols < sp.count * group;
-  }
-  int tiles[PER], items[PER], total = 0, longest = 0;      // of sequences PER lane .. + PER - 1
+  SeqSpan sp[PER];                                         // of sequences PER lane .. + PER - 1
+  int tiles[PER], items[PER], total = 0, longest = 0, all_items = 0;
 #pragma unroll
   for (int i = 0; i < PER; ++i) {
     const int seq = PER * lane + i;
-    const SeqSpan sp = seq_span(b, seq < b.seqs ? seq : 0);
-    const bool any = seq < b.seqs && sp.count;
-    tiles[i] = any ? (sp.n + sp.count + 63) / 64 : 0;
-    items[i] = any ? (sp.count * group + cols - 1) / cols : 0;
+    sp[i] = seq_span(b, seq < b.seqs ? seq : 0);
+    const bool any = seq < b.seqs && sp[i].count;
+    tiles[i] = any ? (sp[i].n + sp[i].count + 63) / 64 : 0;
+    items[i] = any ? (sp[i].count * group + COLS - 1) / COLS : 0;
     longest = tiles[i] > longest ? tiles[i] : longest;
-    total += items[i] * (tiles[i] + kItemTiles);           // (tiles < 2^25, items <= 2^9 of the workgroup's grid: the host holds their product)
-  }
-#pragma unroll
-  for (int o = 32; o; o >>= 1) {
-    const int other = __shfl_xor(longest, o, 64);
-    longest = other > longest ? other : longest;
+    total += items[i] * (tiles[i] + ITEM);                 // (at most what the host has held below 2^30)
+    all_items += items[i];
   }
   total = wave_total(total);
   if (!total) return false;
+  longest = wave_largest(longest);
+  all_items = wave_total(all_items);
   const int room = (int)gridDim.x / b.Hkv;                 // parts of a head
-  int lo = (total + room - 1) / room, hi = longest + kItemTiles;
+  int lo = (total + room - 1) / room, hi = longest + ITEM;
+  // (as many parts as total / T and one more of every item fit at twice the least T)
+  if (2 * all_items <= room && 2 * lo < hi) hi = 2 * lo;
   lo = lo > least ? lo : least;
-  auto parts_of = [&](int tiles_i, int T) { return (tiles_i + kItemTiles + T - 1) / T; };
-  auto parts_at = [&](int T) {
+  int T;
+  float per_T;
+  auto parts_of = [&](int tiles_i) {                       // (tiles_i + ITEM) / T, up
+    const int x = tiles_i + ITEM + T - 1;                  // (the quotient from the reciprocal is off by one at most: x < 2^26, T >= 4)
+    int q = (int)((float)x * per_T), r = x - q * T;
+    q += r >= T ? 1 : r < 0 ? -1 : 0;
+    return q;
+  };
+  auto parts_at = [&](int at_T) {
+    T = at_T;
+    per_T = __builtin_amdgcn_rcpf((float)T);
     int n = 0;
 #pragma unroll
-    for (int i = 0; i < PER; ++i) n += items[i] ? items[i] * parts_of(tiles[i], T) : 0;
+    for (int i = 0; i < PER; ++i) n += items[i] * parts_of(tiles[i]);
     return n;
   };
-  while (lo < hi) {                                        // (at hi every item is one part, and the grid holds all items)
+  while (lo < hi) {                                        // (at longest + ITEM every item is one part, and the grid holds all items)
     const int mid = (lo + hi) / 2;
     if (wave_total(parts_at(mid)) <= room) hi = mid;
     else lo = mid + 1;
   }
-  const int T = lo, mine = parts_at(T);
-  int run = mine;
-#pragma unroll
-  for (int o = 1; o < 64; o <<= 1) {
-    const int other = __shfl_up(run, o, 64);
-    if (lane >= o) run += other;
-  }
-  const int of_head = __builtin_amdgcn_readlane(run, 63);
-  const int per = gridDim.x / 8, w = gridDim.x % 8 ? blockIdx.x : blockIdx.x % 8 * per + blockIdx.x / 8;
+  const int mine = parts_at(lo), run = wave_sums(mine);
+  const int of_head = __builtin_amdgcn_readlane(run, 63), w = place_of_workgroup<(COLS > 32)>();
   if (w >= of_head * b.Hkv) return false;
   const int hk = w / of_head, at = w - hk * of_head;
   const int who = __popcll(__ballot(run <= at));           // the lane whose sequences hold part `at`
-  int rest = at - (run - mine), seq = 0, ct = 0, part = 0, parts = 0, n_tiles = 0;
+  int rest = at - __builtin_amdgcn_readlane(run - mine, who), in_lane = 0;
+  int parts = __builtin_amdgcn_readlane(parts_of(tiles[0]), who), n_tiles = __builtin_amdgcn_readlane(tiles[0], who);
+  SeqSpan of{__builtin_amdgcn_readlane(sp[0].row0, who), __builtin_amdgcn_readlane(sp[0].count, who), __builtin_amdgcn_readlane(sp[0].n, who)};
+  int before = __builtin_amdgcn_readlane(items[0], who) * parts;
 #pragma unroll
-  for (int i = PER - 1; i >= 0; --i) {                     // from the last: the first that `rest` falls into stays
-    int before = 0;
-#pragma unroll
-    for (int k = 0; k < i; ++k) before += items[k] ? items[k] * parts_of(tiles[k], T) : 0;
-    const int p = items[i] ? parts_of(tiles[i], T) : 1, in = rest - before;
-    if (in >= 0 && in < items[i] * p) seq = PER * lane + i, ct = in / p, part = in - ct * p, parts = p, n_tiles = tiles[i];
+  for (int i = 1; i < PER; ++i) {
+    const int p = __builtin_amdgcn_readlane(parts_of(tiles[i]), who), n = __builtin_amdgcn_readlane(items[i], who) * p;
+    if (rest >= before) {                                  // (not in the one before: the last that is taken holds it)
+      rest -= before, before = n, in_lane = i, parts = p, n_tiles = __builtin_amdgcn_readlane(tiles[i], who);
+      of = SeqSpan{__builtin_amdgcn_readlane(sp[i].row0, who), __builtin_amdgcn_readlane(sp[i].count, who), __builtin_amdgcn_readlane(sp[i].n, who)};
+    }
   }
-  seq = __builtin_amdgcn_readlane(seq, who), ct = __builtin_amdgcn_readlane(ct, who), part = __builtin_amdgcn_readlane(part, who);
-  parts = __builtin_amdgcn_readlane(parts, who), n_tiles = __builtin_amdgcn_readlane(n_tiles, who);
-  const SeqSpan sp = seq_span(b, seq);
+  const int ct = rest / parts, part = rest - ct * parts;
   int t0, t1;
   even_share(n_tiles, parts, part, t0, t1);
-  out = Part{seq, hk, ct, t0 * 64, t1 * 64 < sp.n + sp.count ? t1 * 64 : sp.n + sp.count, parts, part, w};
+  out = Part{PER * who + in_lane, hk, ct, t0 * 64, t1 * 64 < of.n + of.count ? t1 * 64 : of.n + of.count, parts, part, w, of};
   return true;
 }
-__device__ __forceinline__ void leave_note(PartNote* notes, int least, bool any, const Part& s) {
+// The same of any batch; least 0: an item to a workgroup
+template <int COLS, int ITEM> __device__ __forceinline__ bool part_of_workgroup(const PagedRows& b, int group, int least, Part& out) {
+  if (least) return b.seqs <= 64 ? share_out<COLS, ITEM, 1>(b, group, least, out) : share_out<COLS, ITEM, kShareSeqs / 64>(b, group, least, out);
+  const SeqSpan sp = seq_span(b, blockIdx.z);
+  out = Part{(int)blockIdx.z, (int)blockIdx.x, (int)blockIdx.y, 0, sp.n + sp.count, 1, 0, 0, sp};
+  return (int)blockIdx.y * COLS < sp.count * group;
+}
+template <bool TILES> __device__ __forceinline__ void leave_note(PartNote* notes, int least, bool any, const Part& s) {
   if (threadIdx.x || !least) return;
-  const int per = gridDim.x / 8, w = gridDim.x % 8 ? blockIdx.x : blockIdx.x % 8 * per + blockIdx.x / 8;
-  notes[w] = any ? PartNote{s.seq, s.hk, s.col_tile, s.part, s.parts, {}} : PartNote{0, 0, 0, 0, 0, {}};
+  notes[place_of_workgroup<TILES>()] = any ? PartNote{s.sp.row0, s.sp.count, s.hk, s.col_tile, s.part, s.parts, {}} : PartNote{};
 }
 
 }  // namespace
@@ -562,16 +579,28 @@ __device__ __forceinline__ void leave_note(PartNote* notes, int least, bool any,
 // K from global memory straight into operand registers, V through 32 rows of LDS of the wavefront's own; the next block is in
 // flight while one is multiplied.  Bound by what the cache streams at.
 template <int HD, int QB>
-__global__ __launch_bounds__(256, 2) void paged_attn_few_kernel(PagedRows b, AttnRows a, int split_len, float* part_o, float* part_ml) {
+__global__ __launch_bounds__(256, 2) void paged_attn_few_kernel(PagedRows b, AttnRows a, int split_len, int least, float* part_o, float* part_ml,
+                                                               PartNote* notes) {
   using Cols = Columns<HD, QB>;
   constexpr int ES = Cols::ES, EB = Cols::EB, PIECES = HD / 8, LOADS = 32 * PIECES / 64, V_BYTES = 32 * HD * 2, STEP = 4 * 32;
   constexpr int O_FLOATS = EB * 4 * 64;
   __shared__ __attribute__((aligned(1024))) unsigned char lds[4 * V_BYTES > 4 * O_FLOATS * 4 ? 4 * V_BYTES : 4 * O_FLOATS * 4];
   __shared__ float lds_m[4 * 64], lds_l[4 * 64];
-  const int seq = blockIdx.z, hk = blockIdx.x, group = a.Hq / b.Hkv, split = blockIdx.y;
-  const SeqSpan sp = seq_span(b, seq);
-  const Slice sl = slice_of(sp, split, split_len);
-  if (sp.count == 0 || sl.key0 >= sl.key1) return;
+  const int group = a.Hq / b.Hkv;
+  constexpr bool SLICES = QB == 1;
+  Part sl;
+  if (SLICES) {
+    const SeqSpan sp = seq_span(b, blockIdx.z);
+    const Slice of = slice_of(sp, blockIdx.y, split_len);
+    if (sp.count == 0 || of.key0 >= of.key1) return;
+    sl = Part{(int)blockIdx.z, (int)blockIdx.x, 0, of.key0, of.key1, of.count, (int)blockIdx.y, 0, sp};
+  } else {
+    const bool any = part_of_workgroup<QB * 16, kFewItem>(b, group, least, sl);
+    leave_note<false>(notes, least, any, sl);
+    if (!any) return;
+  }
+  const int seq = sl.seq, hk = sl.hk;
+  const SeqSpan sp = sl.sp;
   const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, r16 = lane & 15, g = lane >> 4;
   const int S = sp.n + sp.count, in_page = (1 << b.page_shift) - 1;
   const size_t page_elems = (size_t)b.Hkv * HD << b.page_shift, head_elems = (size_t)hk * HD << b.page_shift;
@@ -668,9 +697,6 @@ __global__ __launch_bounds__(256, 2) void paged_attn_few_kernel(PagedRows b, Att
   }
 
   // ---- join the wavefronts
-  const bool split_out = sl.count > 1;
-  float* po = split_out ? part_o + (size_t)split * b.rows * a.Hq * HD : nullptr;
-  float* pml = split_out ? part_ml + (size_t)split * b.rows * a.Hq * 2 : nullptr;
   float* lds_o = (float*)lds;
 #pragma unroll
   for (int qb = 0; qb < QB; ++qb) {
@@ -680,6 +706,7 @@ __global__ __launch_bounds__(256, 2) void paged_attn_few_kernel(PagedRows b, Att
 #pragma unroll
     for (int eb = 0; eb < EB; ++eb) *(floatx4_t*)(lds_o + ((wave * EB + eb) * 64 + lane) * 4) = cols.o[qb][eb];
     __syncthreads();
+    const size_t at = SLICES ? ((size_t)sl.part * b.rows + sp.row0 + cols.row[qb]) * a.Hq + cols.head[qb] : (size_t)sl.place * QB * 16 + qb * 16 + r16;
     float top = -INFINITY, f[4], sum = 0.f;
 #pragma unroll
     for (int w = 0; w < 4; ++w) top = fmaxf(top, lds_m[w * 64 + lane]);
@@ -699,9 +726,10 @@ __global__ __launch_bounds__(256, 2) void paged_attn_few_kernel(PagedRows b, Att
 #pragma unroll
         for (int i = 0; i < 4; ++i) acc[i] = fmaf(f[w], x[i], acc[i]);
       }
-      cols.finish(a, sp, qb, acc, eb + wave, sum, g, po);
+      if (sl.parts == 1) cols.finish(a, sp, qb, acc, eb + wave, sum, g);
+      else if (!SLICES || cols.row[qb] < sp.count) *(floatx4_t*)(part_o + at * HD + (eb + wave) * 16 + g * 4) = acc;
     }
-    if (split_out && wave == 0 && g == 0) cols.finish_sum(a, sp, qb, top, sum, pml);
+    if (sl.parts > 1 && wave == 0 && g == 0 && (!SLICES || cols.row[qb] < sp.count)) *(float2*)(part_ml + at * 2) = make_float2(top, sum);
   }
 }
 
@@ -715,12 +743,12 @@ __global__ __launch_bounds__(64 * NW, 2) void paged_attn_tile_kernel(PagedRows b
   __shared__ int odd;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, group = a.Hq / b.Hkv;
   Part s;
-  const bool any = part_of_workgroup(b, group, COLS, least, s);
-  leave_note(notes, least, any, s);
+  const bool any = part_of_workgroup<COLS, kManyItem>(b, group, least, s);
+  leave_note<true>(notes, least, any, s);
   if (!any) return;
   {
     const int r16 = lane & 15, g = lane >> 4;
-    const SeqSpan sp = seq_span(b, s.seq);
+    const SeqSpan sp = s.sp;
     const int col0 = s.col_tile * COLS + wave * QB * 16;
     const bool works = col0 < sp.count * group;            // the others only bring tiles
     Cols cols;
@@ -750,7 +778,7 @@ __global__ __launch_bounds__(64 * NW, 2) void paged_attn_tile_kernel(PagedRows b
       const float sum = sum_over_groups(cols.l[qb]);
       if (s.parts == 1) {
 #pragma unroll
-        for (int eb = 0; eb < EB; ++eb) cols.finish(a, sp, qb, cols.o[qb][eb], eb, sum, g, nullptr);
+        for (int eb = 0; eb < EB; ++eb) cols.finish(a, sp, qb, cols.o[qb][eb], eb, sum, g);
       } else {
         const size_t at = (size_t)s.place * COLS + (wave * QB + qb) * 16 + r16;
 #pragma unroll
@@ -945,12 +973,12 @@ __global__ __launch_bounds__(256, 2) void paged_attn_wide_kernel(PagedRows b, At
   __shared__ int odd, missing_from;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, group = a.Hq / b.Hkv;
   Part sl;
-  const bool any = part_of_workgroup(b, group, COLS, least, sl);
-  leave_note(notes, least, any, sl);
+  const bool any = part_of_workgroup<COLS, kManyItem>(b, group, least, sl);
+  leave_note<true>(notes, least, any, sl);
   if (!any) return;
   {
     const int half = lane >> 5;
-    const SeqSpan sp = seq_span(b, sl.seq);
+    const SeqSpan sp = sl.sp;
     const int wg_col0 = sl.col_tile * COLS;
     const bool works = wg_col0 + wave * 32 < sp.count * group;             // the others only bring tiles
     const PageView in(b, a, sp, sl.seq, sl.hk);
@@ -1320,11 +1348,10 @@ __global__ __launch_bounds__(256) void paged_attn_share_join_kernel(PagedRows b,
                                                                    const PartNote* notes) {
   const PartNote n = notes[blockIdx.x];
   if (n.parts < 2) return;
-  constexpr int T = HD / 4, UNITS = COLS * T;
-  const SeqSpan sp = seq_span(b, n.seq);
-  const int tid = threadIdx.x, group = a.Hq / b.Hkv;
+  constexpr int T = HD / 4;
+  const int tid = threadIdx.x, group = a.Hq / b.Hkv, left = n.count * group - n.col_tile * COLS;
   int lo, hi;
-  even_share(UNITS, n.parts, n.part, lo, hi);
+  even_share((left < COLS ? left : COLS) * T, n.parts, n.part, lo, hi);
   int width = 256, groups = 1;                             // units and shares of the parts at a time
   while (width / 2 >= hi - lo && width > 8) width /= 2, groups *= 2;
   const int share = tid / width;
@@ -1333,7 +1360,7 @@ __global__ __launch_bounds__(256) void paged_attn_share_join_kernel(PagedRows b,
   auto place = [&](int part) { return (size_t)(blockIdx.x - n.part + part) * COLS; };
   for (int u0 = lo; u0 < hi; u0 += width) {
     const int unit = u0 + tid % width, col = unit / T, e = unit % T * 4, c = n.col_tile * COLS + col, row = c / group;
-    const bool in = unit < hi && row < sp.count;
+    const bool in = unit < hi;
     float top = -INFINITY, sum = 0.f;
     floatx4_t acc = floatx4_t{0.f, 0.f, 0.f, 0.f};
     constexpr int NS = 4;                                  // requested at a time
@@ -1377,7 +1404,7 @@ __global__ __launch_bounds__(256) void paged_attn_share_join_kernel(PagedRows b,
     }
     if (!in || share) continue;
     const float inv = sum == 0.f ? 0.f : 1.0f / sum;
-    ((Loose8*)((bf16_t*)a.out + (int64_t)(sp.row0 + row) * a.out_stride + (int64_t)(n.hk * group + c % group) * HD + e))->v =
+    ((Loose8*)((bf16_t*)a.out + (int64_t)(n.row0 + row) * a.out_stride + (int64_t)(n.hk * group + c % group) * HD + e))->v =
         sum == 0.f ? make_uint2(0, 0) : pack4_bf16(acc[0] * inv, acc[1] * inv, acc[2] * inv, acc[3] * inv);
   }
 }
@@ -1385,56 +1412,50 @@ __global__ __launch_bounds__(256) void paged_attn_share_join_kernel(PagedRows b,
 namespace {
 // How a call runs: from its bounds alone, so that a captured call fits whatever its tables say later
 struct AttnPlan {
-  bool simple, few, f32;
-  int blocks;                    // few: column blocks of 16 (f32: a workgroup each)
-  int split_len, splits;         // few
-  int cols, workgroups, least;   // shared-out work: columns of an item, workgroups (0: one to an item), the least tiles of one
+  bool simple, f32, slices;
+  int blocks, split_len, splits;  // slices: column blocks of 16 (a workgroup each), slices of a sequence
+  int cols, workgroups, least;    // parts: columns of an item, workgroups (0: one to an item), the least tiles of one
 };
 AttnPlan attn_plan(int dtype, const PagedRows& b, int Hq) {
   AttnPlan p{};
   const int cols = b.max_rows * (Hq / b.Hkv), S = b.max_len + b.max_rows;
   p.simple = b.hd != 64 && b.hd != 128;
-  p.split_len = S, p.splits = 1;
   if (p.simple) return p;
   p.f32 = dtype == 0;
-  p.few = p.f32 || cols <= 32;
-  if (p.few) {
-    p.blocks = p.f32 ? (cols + 15) / 16 : cols <= 16 ? 1 : 2;
-    const int64_t groups = (int64_t)b.seqs * b.Hkv * (p.f32 ? p.blocks : 1), want = 1024;
+  p.slices = p.f32 || cols <= 16;
+  if (p.slices) {
+    p.blocks = (cols + 15) / 16;
+    const int64_t groups = (int64_t)b.seqs * b.Hkv * p.blocks;
     const int least = 256;
-    int64_t splits = (want + groups - 1) / groups;
+    int64_t splits = p.f32 ? (1024 + groups - 1) / groups : 512 / groups;
     if (splits > S / least) splits = S / least;
     if (splits < 1) splits = 1;
     p.split_len = (int)(((S + splits - 1) / splits + 63) / 64 * 64);
     p.splits = (S + p.split_len - 1) / p.split_len;
     return p;
   }
-  p.cols = cols <= 64 ? 64 : 128;
+  p.cols = cols <= 32 ? 32 : cols <= 64 ? 64 : 128;
   // two workgroups to a compute unit; a grid that holds every item, or an item to a workgroup where there are many
   const int64_t items = (int64_t)b.seqs * b.Hkv * ((cols + p.cols - 1) / p.cols), tiles = (S + 63) / 64;
-  if (b.seqs <= kShareSeqs && items <= 1024 && items * (tiles + kItemTiles) < 1 << 30) {
-    p.least = 8;
+  const int item = cols <= 32 ? kFewItem : kManyItem, least = cols <= 32 ? 4 : 8;
+  if (b.seqs <= kShareSeqs && items <= 1024 && items * (tiles + item) < 1 << 30 && tiles > 8) {
+    p.least = least;
     p.workgroups = items <= 512 ? 512 : 1024;
     p.workgroups -= p.workgroups % b.Hkv;                  // (every head has room for its items: Hkv <= items)
-    const int64_t most = items * ((tiles + kItemTiles + p.least - 1) / p.least);       // parts
+    const int64_t most = items * ((tiles + item + p.least - 1) / p.least);       // parts
     if (p.workgroups > most) p.workgroups = (int)most;
   }
   return p;
 }
 size_t part_columns(const AttnPlan& p, const PagedRows& b, int Hq) {        // columns of partial results
-  if (p.simple) return 0;
-  if (p.few) return p.splits > 1 ? (size_t)p.splits * b.rows * Hq : 0;
-  return (size_t)p.workgroups * p.cols;
+  return p.slices ? p.splits > 1 ? (size_t)p.splits * b.rows * Hq : 0 : (size_t)p.workgroups * p.cols;
 }
 template <int HD>
 hipError_t launch_attn_hd(const AttnPlan& p, const PagedRows& b, const AttnRows& a, float* part_o, float* part_ml, PartNote* notes, hipStream_t s) {
-  if (p.few) {
-    if (p.f32) {
-      hipLaunchKernelGGL(paged_attn_f32_kernel<HD>, dim3(b.Hkv, p.splits * p.blocks, b.seqs), dim3(256), 0, s, b, a, p.split_len, p.blocks, part_o, part_ml);
-    } else {
-      auto f = p.blocks == 1 ? paged_attn_few_kernel<HD, 1> : paged_attn_few_kernel<HD, 2>;
-      hipLaunchKernelGGL(f, dim3(b.Hkv, p.splits, b.seqs), dim3(256), 0, s, b, a, p.split_len, part_o, part_ml);
-    }
+  if (p.slices) {
+    const dim3 grid(b.Hkv, p.splits * p.blocks, b.seqs);
+    if (p.f32) hipLaunchKernelGGL(paged_attn_f32_kernel<HD>, grid, dim3(256), 0, s, b, a, p.split_len, p.blocks, part_o, part_ml);
+    else hipLaunchKernelGGL((paged_attn_few_kernel<HD, 1>), grid, dim3(256), 0, s, b, a, p.split_len, 0, part_o, part_ml, notes);
     if (p.splits > 1) {
       const bool many = p.splits > 4;
       auto j = p.f32 ? (many ? paged_attn_join_kernel<float, HD, 16> : paged_attn_join_kernel<float, HD, 1>)
@@ -1445,10 +1466,14 @@ hipError_t launch_attn_hd(const AttnPlan& p, const PagedRows& b, const AttnRows&
   }
   const int cols = b.max_rows * (a.Hq / b.Hkv);
   const dim3 grid = p.workgroups ? dim3(p.workgroups) : dim3(b.Hkv, (cols + p.cols - 1) / p.cols, b.seqs);
-  auto f = p.cols == 64 ? paged_attn_tile_kernel<HD, 1, 4> : paged_attn_wide_kernel<HD>;
-  hipLaunchKernelGGL(f, grid, dim3(256), 0, s, b, a, p.least, part_o, part_ml, notes);
-  if (p.workgroups > 1) {
-    auto j = p.cols == 64 ? paged_attn_share_join_kernel<HD, 64> : paged_attn_share_join_kernel<HD, 128>;
+  if (p.cols == 32) {
+    hipLaunchKernelGGL((paged_attn_few_kernel<HD, 2>), grid, dim3(256), 0, s, b, a, 0, p.least, part_o, part_ml, notes);
+  } else {
+    auto f = p.cols == 64 ? paged_attn_tile_kernel<HD, 1, 4> : paged_attn_wide_kernel<HD>;
+    hipLaunchKernelGGL(f, grid, dim3(256), 0, s, b, a, p.least, part_o, part_ml, notes);
+  }
+  if (p.workgroups) {
+    auto j = p.cols == 32 ? paged_attn_share_join_kernel<HD, 32> : p.cols == 64 ? paged_attn_share_join_kernel<HD, 64> : paged_attn_share_join_kernel<HD, 128>;
     hipLaunchKernelGGL(j, dim3(p.workgroups), dim3(256), 0, s, b, a, part_o, part_ml, notes);
   }
   return hipGetLastError();
