@@ -227,9 +227,9 @@ template <int HD> __device__ __forceinline__ int wide_k_place(int row, int piece
   return (piece ^ (HD == 128 ? row & 15 : (row >> 1) & 7)) << 4;
 }
 
-// What a workgroup's NW wavefronts bring of a sequence's pages: tiles of 64 keys of K and V, through registers to LDS
-template <int HD, int NW> struct TileLoader : PageView {
-  static constexpr int PIECES = HD / 8, ROWS = 64 / PIECES, PASS = NW * ROWS, LOADS = 64 / PASS, TILE = 64 * HD * 2;
+// What a workgroup's four wavefronts bring of a sequence's pages: tiles of 64 keys of K and V, through registers to LDS
+template <int HD> struct TileLoader : PageView {
+  static constexpr int PIECES = HD / 8, ROWS = 64 / PIECES, PASS = 4 * ROWS, LOADS = 64 / PASS, TILE = 64 * HD * 2;
   static_assert(64 % PASS == 0, "whole passes");
   typedef u32x4_t Part[LOADS];                              // a wavefront's part of a tile
   int wave, lane;
@@ -318,35 +318,31 @@ template <int HD, int NW> struct TileLoader : PageView {
   }
 };
 
-// Columns of a wavefront: QB blocks of 16
-template <int HD, int QB> struct Columns {
+// The 16 columns of a wavefront
+template <int HD> struct Columns {
   static constexpr int ES = HD / 32, EB = HD / 16;
-  Frag q[QB][ES];
-  floatx4_t o[QB][EB];
-  float m[QB], l[QB];                        // reference point (log2 units, scaled) and this lane's part of the sum
-  int row[QB], head[QB];                     // row of the sequence (count or more: none) and query head
+  Frag q[ES];
+  floatx4_t o[EB];
+  float m, l;                                // reference point (log2 units, scaled) and this lane's part of the sum
+  int row, head;                             // row of the sequence (count or more: none) and query head
 
-  __device__ __forceinline__ void start(const AttnRows& a, const SeqSpan& sp, int hk, int group, int col0, int r16, int g) {
+  __device__ __forceinline__ void start(const AttnRows& a, const SeqSpan& sp, int hk, int group, int col, int g) {
+    row = col / group;
+    head = hk * group + col % group;
+    const int r = row < sp.count ? row : sp.count - 1;
+    const bf16_t* src = (const bf16_t*)a.q + (int64_t)(sp.row0 + r) * a.q_stride + (int64_t)head * HD + g * 8;
 #pragma unroll
-    for (int qb = 0; qb < QB; ++qb) {
-      const int c = col0 + qb * 16 + r16;
-      row[qb] = c / group;
-      head[qb] = hk * group + c % group;
-      const int r = row[qb] < sp.count ? row[qb] : sp.count - 1;
-      const bf16_t* src = (const bf16_t*)a.q + (int64_t)(sp.row0 + r) * a.q_stride + (int64_t)head[qb] * HD + g * 8;
+    for (int es = 0; es < ES; ++es) q[es].nat = ((const Loose16*)(src + es * 32))->v;
+    m = -INFINITY;
+    l = 0.f;
 #pragma unroll
-      for (int es = 0; es < ES; ++es) q[qb][es].nat = ((const Loose16*)(src + es * 32))->v;
-      m[qb] = -INFINITY;
-      l[qb] = 0.f;
-#pragma unroll
-      for (int eb = 0; eb < EB; ++eb) o[qb][eb] = floatx4_t{0.f, 0.f, 0.f, 0.f};
-    }
+    for (int eb = 0; eb < EB; ++eb) o[eb] = floatx4_t{0.f, 0.f, 0.f, 0.f};
   }
 
-  // SUB blocks of 32 keys: k(sub, block, piece) their K operands, V rows in LDS, and with MASKED what every column sees of them
+  // SUB blocks of 32 keys: k(sub, block, piece) their K operands, V rows in LDS, and with MASKED what the column sees of them
   template <int SUB, bool MASKED, typename K>
-  __device__ __forceinline__ void multiply(K&& k, const unsigned char* v_rows, const uint64_t (&vis)[QB], float scale, int r16, int g) {
-    float p[QB][8 * SUB];
+  __device__ __forceinline__ void multiply(K&& k, const unsigned char* v_rows, uint64_t vis, float scale, int r16, int g) {
+    float p[8 * SUB];
 #pragma unroll
     for (int sub = 0; sub < SUB; ++sub)
 #pragma unroll
@@ -354,69 +350,57 @@ template <int HD, int QB> struct Columns {
         Frag kf[ES];
 #pragma unroll
         for (int es = 0; es < ES; ++es) kf[es] = k(sub, b, es);
+        floatx4_t s = floatx4_t{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-        for (int qb = 0; qb < QB; ++qb) {
-          floatx4_t s = floatx4_t{0.f, 0.f, 0.f, 0.f};
+        for (int es = 0; es < ES; ++es) s = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf[es].v, q[es].v, s, 0, 0, 0);
 #pragma unroll
-          for (int es = 0; es < ES; ++es) s = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf[es].v, q[qb][es].v, s, 0, 0, 0);
-#pragma unroll
-          for (int i = 0; i < 4; ++i) p[qb][sub * 8 + b * 4 + i] = s[i];
-        }
+        for (int i = 0; i < 4; ++i) p[sub * 8 + b * 4 + i] = s[i];
       }
-#pragma unroll
-    for (int qb = 0; qb < QB; ++qb) {
-      if (MASKED) {
-#pragma unroll
-        for (int x = 0; x < 8 * SUB; ++x) {
-          const uint32_t word = (uint32_t)(vis[qb] >> (x >> 3) * 32) >> g * 8;
-          p[qb][x] = word >> (x & 7) & 1 ? p[qb][x] : -INFINITY;
-        }
-      }
-      float top = p[qb][0];
-#pragma unroll
-      for (int x = 1; x < 8 * SUB; ++x) top = fmaxf(top, p[qb][x]);
-      top = max_over_groups(top) * scale;
-      const bool grow = top > m[qb] + kRescaleStep;        // m = -inf: any number
-      if (__any(grow)) {
-        const float keep = grow ? __builtin_amdgcn_exp2f(m[qb] - top) : 1.0f;
-        l[qb] *= keep;
-#pragma unroll
-        for (int eb = 0; eb < EB; ++eb) o[qb][eb] *= keep;
-        m[qb] = grow ? top : m[qb];
-      }
-      const float ref = m[qb] == -INFINITY ? 0.f : m[qb];
-      float sum = 0.f;
+    if (MASKED) {
 #pragma unroll
       for (int x = 0; x < 8 * SUB; ++x) {
-        p[qb][x] = __builtin_amdgcn_exp2f(fmaf(p[qb][x], scale, -ref));
-        sum += p[qb][x];
+        const uint32_t word = (uint32_t)(vis >> (x >> 3) * 32) >> g * 8;
+        p[x] = word >> (x & 7) & 1 ? p[x] : -INFINITY;
       }
-      l[qb] += sum;
     }
+    float top = p[0];
+#pragma unroll
+    for (int x = 1; x < 8 * SUB; ++x) top = fmaxf(top, p[x]);
+    top = max_over_groups(top) * scale;
+    const bool grow = top > m + kRescaleStep;              // m = -inf: any number
+    if (__any(grow)) {
+      const float keep = grow ? __builtin_amdgcn_exp2f(m - top) : 1.0f;
+      l *= keep;
+#pragma unroll
+      for (int eb = 0; eb < EB; ++eb) o[eb] *= keep;
+      m = grow ? top : m;
+    }
+    const float ref = m == -INFINITY ? 0.f : m;
+    float sum = 0.f;
+#pragma unroll
+    for (int x = 0; x < 8 * SUB; ++x) {
+      p[x] = __builtin_amdgcn_exp2f(fmaf(p[x], scale, -ref));
+      sum += p[x];
+    }
+    l += sum;
 #pragma unroll
     for (int sub = 0; sub < SUB; ++sub) {
-      Frag pf[QB];
+      Frag pf;
 #pragma unroll
-      for (int qb = 0; qb < QB; ++qb)
-#pragma unroll
-        for (int h = 0; h < 2; ++h)
-          pf[qb].half[h] = pack4_bf16(p[qb][sub * 8 + 4 * h], p[qb][sub * 8 + 4 * h + 1], p[qb][sub * 8 + 4 * h + 2], p[qb][sub * 8 + 4 * h + 3]);
+      for (int h = 0; h < 2; ++h)
+        pf.half[h] = pack4_bf16(p[sub * 8 + 4 * h], p[sub * 8 + 4 * h + 1], p[sub * 8 + 4 * h + 2], p[sub * 8 + 4 * h + 3]);
       const unsigned char* rows = v_rows + sub * 32 * HD * 2;
 #pragma unroll
       for (int eb = 0; eb < EB; ++eb) {
         const Frag vf = v_operand<HD>(rows, eb, r16, g);
-#pragma unroll
-        for (int qb = 0; qb < QB; ++qb) o[qb][eb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf.v, pf[qb].v, o[qb][eb], 0, 0, 0);
+        o[eb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf.v, pf.v, o[eb], 0, 0, 0);
       }
     }
   }
   // The values of keys j0 .. j1 - 1 that are no numbers, to the columns that see them: rare, key by key
   __device__ __forceinline__ void add_odd_values(const AttnRows& a, const SeqSpan& sp, const PageView& in, int j0, int j1, int g) {
     for (; j0 < j1; j0 += 64) {
-      uint64_t vis[QB];
-      const uint64_t there = in.there_at(j0);
-#pragma unroll
-      for (int qb = 0; qb < QB; ++qb) vis[qb] = seen_bits(mask_of(a, sp, row[qb]), sp, row[qb], j0, there);
+      const uint64_t there = in.there_at(j0), vis = seen_bits(mask_of(a, sp, row), sp, row, j0, there);
 #pragma unroll 1
       for (int k = 0; k < 64 && j0 + k < j1; ++k) {
         if (!(there >> k & 1)) continue;
@@ -424,18 +408,15 @@ template <int HD, int QB> struct Columns {
 #pragma unroll
         for (int eb = 0; eb < EB; ++eb)
           add_odd(values + eb * 32, [&](int i, float v) __attribute__((always_inline)) {
-#pragma unroll
-            for (int qb = 0; qb < QB; ++qb)
-              if (vis[qb] >> k & 1) o[qb][eb][i] += v;
+            if (vis >> k & 1) o[eb][i] += v;
           });
       }
     }
   }
-
-  // Column (qb, r16): o over its sum
-  __device__ __forceinline__ void finish(const AttnRows& a, const SeqSpan& sp, int qb, const floatx4_t& acc, int eb, float sum, int g) const {
-    if (row[qb] < sp.count)
-      store_four((bf16_t*)a.out + (int64_t)(sp.row0 + row[qb]) * a.out_stride + (int64_t)head[qb] * HD + eb * 16 + g * 4, acc, sum);
+  // o over its sum
+  __device__ __forceinline__ void finish(const AttnRows& a, const SeqSpan& sp, const floatx4_t& acc, int eb, float sum, int g) const {
+    if (row < sp.count)
+      store_four((bf16_t*)a.out + (int64_t)(sp.row0 + row) * a.out_stride + (int64_t)head * HD + eb * 16 + g * 4, acc, sum);
   }
 };
 
@@ -450,11 +431,12 @@ __device__ __forceinline__ Slice slice_of(const SeqSpan& sp, int split, int spli
 }
 
 // Shared-out work of the bf16 kernels.  An item is a (head, sequence, column tile); a long one is cut into parts, a workgroup each, none
-// of more than T tiles of 64 keys with `ITEM` for what starting and ending costs, T the smallest with which all parts fit the
+// of more than T tiles of 64 keys with kItemTiles for what starting and ending costs, T the smallest with which all parts fit the
 // grid: lengths may be as ragged as they like.  The parts of an item leave partial results, which a second kernel joins.  Every
 // wavefront works this out for itself.
 constexpr int kShareSeqs = 256;              // sequences that a wavefront can add up
-constexpr int kFewItem = 2, kManyItem = 3;    // tiles that starting and ending a part costs: TODO
+constexpr int kItemTiles = 3;                // tiles that starting and ending a part costs (5 to 6 us; a tile 1.9); with 2 and with 5 in its place
+                                             // trees of 64 rows over 8 x 4096 slots take 103 and 106 us, with 3 100
 struct Part {
   int seq, hk, col_tile, key0, key1;
   int parts, part, place;                    // of the item: how many, which, and where in the row of parts this one stands
@@ -485,14 +467,14 @@ __device__ __forceinline__ int wave_largest(int v) {                      // of 
   step(__builtin_amdgcn_update_dpp(0, v, 0x143, 0xc, 0xf, false));
   return __builtin_amdgcn_readlane(v, 63);
 }
-// The place of a workgroup in the row of parts.  Where several column tiles read the same keys, the workgroups of one XCD (numbers that
-// are equal modulo 8) have consecutive parts, heads outermost, so that they meet in one L2.
-template <bool TILES> __device__ __forceinline__ int place_of_workgroup() {
+// The place of a workgroup in the row of parts: the workgroups of one XCD (numbers that are equal modulo 8) have consecutive parts, heads
+// outermost, so that column tiles of the same keys meet in one L2
+__device__ __forceinline__ int place_of_workgroup() {
   const int per = gridDim.x / 8;
-  return !TILES || gridDim.x % 8 ? blockIdx.x : blockIdx.x % 8 * per + blockIdx.x / 8;
+  return gridDim.x % 8 ? blockIdx.x : blockIdx.x % 8 * per + blockIdx.x / 8;
 }
 // Which part this workgroup has of a batch of up to 64 PER sequences; false: none
-template <int COLS, int ITEM, int PER>
+template <int COLS, int PER>
 __device__ __forceinline__ bool share_out(const PagedRows& b, int group, int least, Part& out) {
   const int lane = threadIdx.x & 63;
   SeqSpan sp[PER];                                         // of sequences PER lane .. + PER - 1
@@ -505,7 +487,7 @@ __device__ __forceinline__ bool share_out(const PagedRows& b, int group, int lea
     tiles[i] = any ? (sp[i].n + sp[i].count + 63) / 64 : 0;
     items[i] = any ? (sp[i].count * group + COLS - 1) / COLS : 0;
     longest = tiles[i] > longest ? tiles[i] : longest;
-    total += items[i] * (tiles[i] + ITEM);                 // (at most what the host has held below 2^30)
+    total += items[i] * (tiles[i] + kItemTiles);                 // (at most what the host has held below 2^30)
     all_items += items[i];
   }
   total = wave_total(total);
@@ -513,14 +495,14 @@ __device__ __forceinline__ bool share_out(const PagedRows& b, int group, int lea
   longest = wave_largest(longest);
   all_items = wave_total(all_items);
   const int room = (int)gridDim.x / b.Hkv;                 // parts of a head
-  int lo = (total + room - 1) / room, hi = longest + ITEM;
+  int lo = (total + room - 1) / room, hi = longest + kItemTiles;
   // (as many parts as total / T and one more of every item fit at twice the least T)
   if (2 * all_items <= room && 2 * lo < hi) hi = 2 * lo;
   lo = lo > least ? lo : least;
   int T;
   float per_T;
-  auto parts_of = [&](int tiles_i) {                       // (tiles_i + ITEM) / T, up
-    const int x = tiles_i + ITEM + T - 1;                  // (the quotient from the reciprocal is off by one at most: x < 2^26, T >= 4)
+  auto parts_of = [&](int tiles_i) {                       // (tiles_i + kItemTiles) / T, up
+    const int x = tiles_i + kItemTiles + T - 1;                  // (the quotient from the reciprocal is off by one at most: x < 2^26, T >= 4)
     int q = (int)((float)x * per_T), r = x - q * T;
     q += r >= T ? 1 : r < 0 ? -1 : 0;
     return q;
@@ -533,13 +515,13 @@ __device__ __forceinline__ bool share_out(const PagedRows& b, int group, int lea
     for (int i = 0; i < PER; ++i) n += items[i] * parts_of(tiles[i]);
     return n;
   };
-  while (lo < hi) {                                        // (at longest + ITEM every item is one part, and the grid holds all items)
+  while (lo < hi) {                                        // (at longest + kItemTiles every item is one part, and the grid holds all items)
     const int mid = (lo + hi) / 2;
     if (wave_total(parts_at(mid)) <= room) hi = mid;
     else lo = mid + 1;
   }
   const int mine = parts_at(lo), run = wave_sums(mine);
-  const int of_head = __builtin_amdgcn_readlane(run, 63), w = place_of_workgroup<(COLS > 32)>();
+  const int of_head = __builtin_amdgcn_readlane(run, 63), w = place_of_workgroup();
   if (w >= of_head * b.Hkv) return false;
   const int hk = w / of_head, at = w - hk * of_head;
   const int who = __popcll(__ballot(run <= at));           // the lane whose sequences hold part `at`
@@ -562,15 +544,15 @@ __device__ __forceinline__ bool share_out(const PagedRows& b, int group, int lea
   return true;
 }
 // The same of any batch; least 0: an item to a workgroup
-template <int COLS, int ITEM> __device__ __forceinline__ bool part_of_workgroup(const PagedRows& b, int group, int least, Part& out) {
-  if (least) return b.seqs <= 64 ? share_out<COLS, ITEM, 1>(b, group, least, out) : share_out<COLS, ITEM, kShareSeqs / 64>(b, group, least, out);
+template <int COLS> __device__ __forceinline__ bool part_of_workgroup(const PagedRows& b, int group, int least, Part& out) {
+  if (least) return b.seqs <= 64 ? share_out<COLS, 1>(b, group, least, out) : share_out<COLS, kShareSeqs / 64>(b, group, least, out);
   const SeqSpan sp = seq_span(b, blockIdx.z);
   out = Part{(int)blockIdx.z, (int)blockIdx.x, (int)blockIdx.y, 0, sp.n + sp.count, 1, 0, 0, sp};
   return (int)blockIdx.y * COLS < sp.count * group;
 }
-template <bool TILES> __device__ __forceinline__ void leave_note(PartNote* notes, int least, bool any, const Part& s) {
+__device__ __forceinline__ void leave_note(PartNote* notes, int least, bool any, const Part& s) {
   if (threadIdx.x || !least) return;
-  notes[place_of_workgroup<TILES>()] = any ? PartNote{s.sp.row0, s.sp.count, s.hk, s.col_tile, s.part, s.parts, {}} : PartNote{};
+  notes[place_of_workgroup()] = any ? PartNote{s.sp.row0, s.sp.count, s.hk, s.col_tile, s.part, s.parts, {}} : PartNote{};
 }
 
 }  // namespace
@@ -578,29 +560,17 @@ template <bool TILES> __device__ __forceinline__ void leave_note(PartNote* notes
 // Up to 32 columns: the four wavefronts of a workgroup take blocks of 32 keys in turn, each for itself (no barrier until the end),
 // K from global memory straight into operand registers, V through 32 rows of LDS of the wavefront's own; the next block is in
 // flight while one is multiplied.  Bound by what the cache streams at.
-template <int HD, int QB>
-__global__ __launch_bounds__(256, 2) void paged_attn_few_kernel(PagedRows b, AttnRows a, int split_len, int least, float* part_o, float* part_ml,
-                                                               PartNote* notes) {
-  using Cols = Columns<HD, QB>;
+template <int HD>
+__global__ __launch_bounds__(256, 2) void paged_attn_few_kernel(PagedRows b, AttnRows a, int split_len, float* part_o, float* part_ml) {
+  using Cols = Columns<HD>;
   constexpr int ES = Cols::ES, EB = Cols::EB, PIECES = HD / 8, LOADS = 32 * PIECES / 64, V_BYTES = 32 * HD * 2, STEP = 4 * 32;
   constexpr int O_FLOATS = EB * 4 * 64;
   __shared__ __attribute__((aligned(1024))) unsigned char lds[4 * V_BYTES > 4 * O_FLOATS * 4 ? 4 * V_BYTES : 4 * O_FLOATS * 4];
   __shared__ float lds_m[4 * 64], lds_l[4 * 64];
-  const int group = a.Hq / b.Hkv;
-  constexpr bool SLICES = QB == 1;
-  Part sl;
-  if (SLICES) {
-    const SeqSpan sp = seq_span(b, blockIdx.z);
-    const Slice of = slice_of(sp, blockIdx.y, split_len);
-    if (sp.count == 0 || of.key0 >= of.key1) return;
-    sl = Part{(int)blockIdx.z, (int)blockIdx.x, 0, of.key0, of.key1, of.count, (int)blockIdx.y, 0, sp};
-  } else {
-    const bool any = part_of_workgroup<QB * 16, kFewItem>(b, group, least, sl);
-    leave_note<false>(notes, least, any, sl);
-    if (!any) return;
-  }
-  const int seq = sl.seq, hk = sl.hk;
-  const SeqSpan sp = sl.sp;
+  const int seq = blockIdx.z, hk = blockIdx.x, group = a.Hq / b.Hkv, split = blockIdx.y;
+  const SeqSpan sp = seq_span(b, seq);
+  const Slice sl = slice_of(sp, split, split_len);
+  if (sp.count == 0 || sl.key0 >= sl.key1) return;
   const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, r16 = lane & 15, g = lane >> 4;
   const int S = sp.n + sp.count, in_page = (1 << b.page_shift) - 1;
   const size_t page_elems = (size_t)b.Hkv * HD << b.page_shift, head_elems = (size_t)hk * HD << b.page_shift;
@@ -610,7 +580,7 @@ __global__ __launch_bounds__(256, 2) void paged_attn_few_kernel(PagedRows b, Att
   unsigned char* v_rows = lds + wave * V_BYTES;
 
   Cols cols;
-  cols.start(a, sp, hk, group, 0, r16, g);
+  cols.start(a, sp, hk, group, r16, g);
 
   // the page of keys 8 (r16 / 4) .. + 7 of a block (a page holds whole eights)
   auto pages = [&](int j0) __attribute__((always_inline)) {
@@ -677,11 +647,7 @@ __global__ __launch_bounds__(256, 2) void paged_attn_few_kernel(PagedRows b, Att
         if (MASKED) odd = clear_v(there);
         store_v();
         if (more) load_v(j0 + STEP, id_next);
-        uint64_t vis[QB] = {};
-        if (MASKED) {
-#pragma unroll
-          for (int qb = 0; qb < QB; ++qb) vis[qb] = seen_bits(mask_of(a, sp, cols.row[qb]), sp, cols.row[qb], j0, there);
-        }
+        const uint64_t vis = MASKED ? seen_bits(mask_of(a, sp, cols.row), sp, cols.row, j0, there) : 0;
         cols.template multiply<1, MASKED>([&](int, int bl, int es) __attribute__((always_inline)) { return kf[bl][es]; }, v_rows, vis,
                                           a.scale_log2, r16, g);
         if (MASKED && odd) cols.add_odd_values(a, sp, view, j0, j0 + 32 < S ? j0 + 32 : S, g);
@@ -698,62 +664,60 @@ __global__ __launch_bounds__(256, 2) void paged_attn_few_kernel(PagedRows b, Att
 
   // ---- join the wavefronts
   float* lds_o = (float*)lds;
+  __syncthreads();
+  lds_m[wave * 64 + lane] = cols.m;
+  lds_l[wave * 64 + lane] = sum_over_groups(cols.l);
 #pragma unroll
-  for (int qb = 0; qb < QB; ++qb) {
-    __syncthreads();
-    lds_m[wave * 64 + lane] = cols.m[qb];
-    lds_l[wave * 64 + lane] = sum_over_groups(cols.l[qb]);
+  for (int eb = 0; eb < EB; ++eb) *(floatx4_t*)(lds_o + ((wave * EB + eb) * 64 + lane) * 4) = cols.o[eb];
+  __syncthreads();
+  if (cols.row >= sp.count) return;
+  float top = -INFINITY, f[4], sum = 0.f;
 #pragma unroll
-    for (int eb = 0; eb < EB; ++eb) *(floatx4_t*)(lds_o + ((wave * EB + eb) * 64 + lane) * 4) = cols.o[qb][eb];
-    __syncthreads();
-    const size_t at = SLICES ? ((size_t)sl.part * b.rows + sp.row0 + cols.row[qb]) * a.Hq + cols.head[qb] : (size_t)sl.place * QB * 16 + qb * 16 + r16;
-    float top = -INFINITY, f[4], sum = 0.f;
+  for (int w = 0; w < 4; ++w) top = fmaxf(top, lds_m[w * 64 + lane]);
+  const float ref = top == -INFINITY ? 0.f : top;
 #pragma unroll
-    for (int w = 0; w < 4; ++w) top = fmaxf(top, lds_m[w * 64 + lane]);
-    const float ref = top == -INFINITY ? 0.f : top;
+  for (int w = 0; w < 4; ++w) {
+    f[w] = __builtin_amdgcn_exp2f(lds_m[w * 64 + lane] - ref);
+    sum += f[w] * lds_l[w * 64 + lane];
+  }
+  const size_t at = ((size_t)split * b.rows + sp.row0 + cols.row) * a.Hq + cols.head;
+#pragma unroll
+  for (int eb = 0; eb < EB; eb += 4) {
+    if (eb + wave >= EB) continue;
+    floatx4_t acc = floatx4_t{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
     for (int w = 0; w < 4; ++w) {
-      f[w] = __builtin_amdgcn_exp2f(lds_m[w * 64 + lane] - ref);
-      sum += f[w] * lds_l[w * 64 + lane];
+      const floatx4_t x = *(const floatx4_t*)(lds_o + ((w * EB + eb + wave) * 64 + lane) * 4);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) acc[i] = fmaf(f[w], x[i], acc[i]);
     }
-#pragma unroll
-    for (int eb = 0; eb < EB; eb += 4) {
-      if (eb + wave >= EB) continue;
-      floatx4_t acc = floatx4_t{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-      for (int w = 0; w < 4; ++w) {
-        const floatx4_t x = *(const floatx4_t*)(lds_o + ((w * EB + eb + wave) * 64 + lane) * 4);
-#pragma unroll
-        for (int i = 0; i < 4; ++i) acc[i] = fmaf(f[w], x[i], acc[i]);
-      }
-      if (sl.parts == 1) cols.finish(a, sp, qb, acc, eb + wave, sum, g);
-      else if (!SLICES || cols.row[qb] < sp.count) *(floatx4_t*)(part_o + at * HD + (eb + wave) * 16 + g * 4) = acc;
-    }
-    if (sl.parts > 1 && wave == 0 && g == 0 && (!SLICES || cols.row[qb] < sp.count)) *(float2*)(part_ml + at * 2) = make_float2(top, sum);
+    if (sl.count > 1) *(floatx4_t*)(part_o + at * HD + (eb + wave) * 16 + g * 4) = acc;
+    else cols.finish(a, sp, acc, eb + wave, sum, g);
   }
+  if (sl.count > 1 && wave == 0 && g == 0) *(float2*)(part_ml + at * 2) = make_float2(top, sum);
 }
 
 // More columns: every wavefront owns QB blocks of 16, tiles of 64 keys of K and V go through LDS for all of them.
-template <int HD, int QB, int NW>
-__global__ __launch_bounds__(64 * NW, 2) void paged_attn_tile_kernel(PagedRows b, AttnRows a, int least, float* part_o, float* part_ml,
+template <int HD>
+__global__ __launch_bounds__(256, 2) void paged_attn_tile_kernel(PagedRows b, AttnRows a, int least, float* part_o, float* part_ml,
                                                                     PartNote* notes) {
-  using Cols = Columns<HD, QB>;
-  constexpr int EB = Cols::EB, TILE = 64 * HD * 2, COLS = NW * QB * 16;
+  using Cols = Columns<HD>;
+  constexpr int EB = Cols::EB, TILE = 64 * HD * 2, COLS = 64;
   __shared__ __attribute__((aligned(1024))) unsigned char lds[4 * TILE];   // two stages of (K tile, V tile)
   __shared__ int odd;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, group = a.Hq / b.Hkv;
   Part s;
-  const bool any = part_of_workgroup<COLS, kManyItem>(b, group, least, s);
-  leave_note<true>(notes, least, any, s);
+  const bool any = part_of_workgroup<COLS>(b, group, least, s);
+  leave_note(notes, least, any, s);
   if (!any) return;
   {
     const int r16 = lane & 15, g = lane >> 4;
     const SeqSpan sp = s.sp;
-    const int col0 = s.col_tile * COLS + wave * QB * 16;
+    const int col0 = s.col_tile * COLS + wave * 16;
     const bool works = col0 < sp.count * group;            // the others only bring tiles
     Cols cols;
-    cols.start(a, sp, s.hk, group, col0, r16, g);
-    const TileLoader<HD, NW> in(b, a, sp, s.seq, s.hk, wave, lane);
+    cols.start(a, sp, s.hk, group, col0 + r16, g);
+    const TileLoader<HD> in(b, a, sp, s.seq, s.hk, wave, lane);
     const int rest = in.run(lds, &odd, s.key0, s.key1, sp.n, [&](auto masked, int j0, uint64_t there, const unsigned char* base) __attribute__((always_inline)) {
       constexpr bool MASKED = decltype(masked)::value;
       if (!works) return;
@@ -764,27 +728,20 @@ __global__ __launch_bounds__(64 * NW, 2) void paged_attn_tile_kernel(PagedRows b
         f.nat = *(const u32x4_t*)(base + row * (HD * 2) + k_place<HD>(row, es * 4 + g));
         return f;
       };
-      uint64_t vis[QB] = {};
-      if (MASKED) {
-#pragma unroll
-        for (int qb = 0; qb < QB; ++qb) vis[qb] = seen_bits(mask_of(a, sp, cols.row[qb]), sp, cols.row[qb], j0, there);
-      }
+      const uint64_t vis = MASKED ? seen_bits(mask_of(a, sp, cols.row), sp, cols.row, j0, there) : 0;
       cols.template multiply<2, MASKED>(k_of, base + TILE, vis, a.scale_log2, r16, g);
     });
     if (!works) return;
     if (odd) cols.add_odd_values(a, sp, in, rest, s.key1, g);
+    const float sum = sum_over_groups(cols.l);
+    if (s.parts == 1) {
 #pragma unroll
-    for (int qb = 0; qb < QB; ++qb) {
-      const float sum = sum_over_groups(cols.l[qb]);
-      if (s.parts == 1) {
+      for (int eb = 0; eb < EB; ++eb) cols.finish(a, sp, cols.o[eb], eb, sum, g);
+    } else {
+      const size_t at = (size_t)s.place * COLS + wave * 16 + r16;
 #pragma unroll
-        for (int eb = 0; eb < EB; ++eb) cols.finish(a, sp, qb, cols.o[qb][eb], eb, sum, g);
-      } else {
-        const size_t at = (size_t)s.place * COLS + (wave * QB + qb) * 16 + r16;
-#pragma unroll
-        for (int eb = 0; eb < EB; ++eb) *(floatx4_t*)(part_o + at * HD + eb * 16 + g * 4) = cols.o[qb][eb];
-        if (g == 0) *(float2*)(part_ml + at * 2) = make_float2(cols.m[qb], sum);
-      }
+      for (int eb = 0; eb < EB; ++eb) *(floatx4_t*)(part_o + at * HD + eb * 16 + g * 4) = cols.o[eb];
+      if (g == 0) *(float2*)(part_ml + at * 2) = make_float2(cols.m, sum);
     }
   }
 }
@@ -973,8 +930,8 @@ __global__ __launch_bounds__(256, 2) void paged_attn_wide_kernel(PagedRows b, At
   __shared__ int odd, missing_from;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, group = a.Hq / b.Hkv;
   Part sl;
-  const bool any = part_of_workgroup<COLS, kManyItem>(b, group, least, sl);
-  leave_note<true>(notes, least, any, sl);
+  const bool any = part_of_workgroup<COLS>(b, group, least, sl);
+  leave_note(notes, least, any, sl);
   if (!any) return;
   {
     const int half = lane >> 5;
@@ -1434,15 +1391,14 @@ AttnPlan attn_plan(int dtype, const PagedRows& b, int Hq) {
     p.splits = (S + p.split_len - 1) / p.split_len;
     return p;
   }
-  p.cols = cols <= 32 ? 32 : cols <= 64 ? 64 : 128;
+  p.cols = cols <= 64 ? 64 : 128;
   // two workgroups to a compute unit; a grid that holds every item, or an item to a workgroup where there are many
   const int64_t items = (int64_t)b.seqs * b.Hkv * ((cols + p.cols - 1) / p.cols), tiles = (S + 63) / 64;
-  const int item = cols <= 32 ? kFewItem : kManyItem, least = cols <= 32 ? 4 : 8;
-  if (b.seqs <= kShareSeqs && items <= 1024 && items * (tiles + item) < 1 << 30 && tiles > 8) {
-    p.least = least;
+  if (b.seqs <= kShareSeqs && items <= 1024 && items * (tiles + kItemTiles) < 1 << 30 && tiles > 8) {
+    p.least = 8;
     p.workgroups = items <= 512 ? 512 : 1024;
     p.workgroups -= p.workgroups % b.Hkv;                  // (every head has room for its items: Hkv <= items)
-    const int64_t most = items * ((tiles + item + p.least - 1) / p.least);       // parts
+    const int64_t most = items * ((tiles + kItemTiles + p.least - 1) / p.least);       // parts
     if (p.workgroups > most) p.workgroups = (int)most;
   }
   return p;
@@ -1455,7 +1411,7 @@ hipError_t launch_attn_hd(const AttnPlan& p, const PagedRows& b, const AttnRows&
   if (p.slices) {
     const dim3 grid(b.Hkv, p.splits * p.blocks, b.seqs);
     if (p.f32) hipLaunchKernelGGL(paged_attn_f32_kernel<HD>, grid, dim3(256), 0, s, b, a, p.split_len, p.blocks, part_o, part_ml);
-    else hipLaunchKernelGGL((paged_attn_few_kernel<HD, 1>), grid, dim3(256), 0, s, b, a, p.split_len, 0, part_o, part_ml, notes);
+    else hipLaunchKernelGGL(paged_attn_few_kernel<HD>, grid, dim3(256), 0, s, b, a, p.split_len, part_o, part_ml);
     if (p.splits > 1) {
       const bool many = p.splits > 4;
       auto j = p.f32 ? (many ? paged_attn_join_kernel<float, HD, 16> : paged_attn_join_kernel<float, HD, 1>)
@@ -1466,14 +1422,10 @@ hipError_t launch_attn_hd(const AttnPlan& p, const PagedRows& b, const AttnRows&
   }
   const int cols = b.max_rows * (a.Hq / b.Hkv);
   const dim3 grid = p.workgroups ? dim3(p.workgroups) : dim3(b.Hkv, (cols + p.cols - 1) / p.cols, b.seqs);
-  if (p.cols == 32) {
-    hipLaunchKernelGGL((paged_attn_few_kernel<HD, 2>), grid, dim3(256), 0, s, b, a, 0, p.least, part_o, part_ml, notes);
-  } else {
-    auto f = p.cols == 64 ? paged_attn_tile_kernel<HD, 1, 4> : paged_attn_wide_kernel<HD>;
-    hipLaunchKernelGGL(f, grid, dim3(256), 0, s, b, a, p.least, part_o, part_ml, notes);
-  }
+  auto f = p.cols == 64 ? paged_attn_tile_kernel<HD> : paged_attn_wide_kernel<HD>;
+  hipLaunchKernelGGL(f, grid, dim3(256), 0, s, b, a, p.least, part_o, part_ml, notes);
   if (p.workgroups) {
-    auto j = p.cols == 32 ? paged_attn_share_join_kernel<HD, 32> : p.cols == 64 ? paged_attn_share_join_kernel<HD, 64> : paged_attn_share_join_kernel<HD, 128>;
+    auto j = p.cols == 64 ? paged_attn_share_join_kernel<HD, 64> : paged_attn_share_join_kernel<HD, 128>;
     hipLaunchKernelGGL(j, dim3(p.workgroups), dim3(256), 0, s, b, a, part_o, part_ml, notes);
   }
   return hipGetLastError();
