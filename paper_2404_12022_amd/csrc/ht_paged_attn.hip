@@ -9,17 +9,22 @@
 
 namespace ht {
 
-// Any head width, either type: a wavefront per (row, query head), a lane per key for the scores and per output element for the
-// values.  Keys and values that a row does not see are read but never used: what they hold does not matter.
-template <typename T>
-__global__ __launch_bounds__(64) void paged_attn_simple_kernel(PagedRows b, AttnRows a) {
-  __shared__ float qs[256];
-  const int seq = blockIdx.z, i = blockIdx.y, h = blockIdx.x, lane = threadIdx.x;
+// Any head width, either type: a workgroup per (row, query head), whose wavefronts take blocks of 64 keys in turn, a lane per key for the
+// scores and per output element for the values.  Keys and values that a row does not see are read but never used: what they hold
+// does not matter.  Every row reads its sequence's cache for itself and multiplies on the vector units, so this is for
+// heads that the matrix kernels below do not take (8 sequences of 1000, 8 heads of 80: 29 us for a row each, 310 us for 64).
+template <typename T, int WAVES>
+__global__ __launch_bounds__(64 * WAVES) void paged_attn_simple_kernel(PagedRows b, AttnRows a) {
+  __shared__ float qs[256], lds_o[WAVES][256], lds_m[WAVES], lds_l[WAVES];
+  struct Pair {
+    T v[2];
+  };
+  const int seq = blockIdx.z, i = blockIdx.y, h = blockIdx.x, wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
   const SeqSpan sp = seq_span(b, seq);
   if (i >= sp.count) return;
   const int row = sp.row0 + i, hk = h / (a.Hq / b.Hkv), hd = b.hd, in_page = (1 << b.page_shift) - 1;
   const T* q = (const T*)a.q + row * a.q_stride + (size_t)h * hd;
-  for (int e = lane; e < hd; e += 64) qs[e] = Conv<T>::load(q + e) * a.scale_log2;
+  for (int e = threadIdx.x; e < hd; e += 64 * WAVES) qs[e] = Conv<T>::load(q + e) * a.scale_log2;
   uint64_t mask[kMaskWords];
 #pragma unroll
   for (int w = 0; w < kMaskWords; ++w) {
@@ -27,10 +32,10 @@ __global__ __launch_bounds__(64) void paged_attn_simple_kernel(PagedRows b, Attn
     mask[w] = a.anc ? a.anc[(size_t)row * kMaskWords + w] : past >= 64 ? ~0ull : past > 0 ? (1ull << past) - 1 : 0ull;
   }
   __syncthreads();
-  constexpr int EL = 4;
+  constexpr int EL = 4, AT_ONCE = 8;                       // keys whose values are requested together
   float acc[EL] = {}, top = -INFINITY, sum = 0.f;
   const int S = sp.n + sp.count;
-  for (int j0 = 0; j0 < S; j0 += 64) {
+  for (int j0 = wave * 64; j0 < S; j0 += 64 * WAVES) {
     const int j = j0 + lane;
     const int page = j < S ? page_of(b, seq, j) : -1;
     const size_t at = ((((size_t)(page < 0 ? 0 : page) * b.Hkv + hk) << b.page_shift) + (j & in_page)) * hd;
@@ -44,9 +49,13 @@ __global__ __launch_bounds__(64) void paged_attn_simple_kernel(PagedRows b, Attn
     }
     float z = -INFINITY;
     if (seen) {
-      const T* k = (const T*)a.k_pages + at;
+      const Pair* k = (const Pair*)((const T*)a.k_pages + at);         // (heads are even, pages on 16 bytes)
       z = 0.f;
-      for (int e = 0; e < hd; ++e) z = fmaf(qs[e], Conv<T>::load(k + e), z);
+#pragma unroll 8
+      for (int e = 0; e < hd / 2; ++e) {
+        const Pair x = k[e];
+        z = fmaf(qs[2 * e], Conv<T>::load(&x.v[0]), fmaf(qs[2 * e + 1], Conv<T>::load(&x.v[1]), z));
+      }
     }
     float best = z;
     for (int o = 32; o; o >>= 1) best = fmaxf(best, __shfl_xor(best, o, 64));
@@ -57,21 +66,41 @@ __global__ __launch_bounds__(64) void paged_attn_simple_kernel(PagedRows b, Attn
 #pragma unroll
     for (int t = 0; t < EL; ++t) acc[t] *= keep;
     const unsigned long long any = __ballot(seen);
-    for (int l = 0; l < 64; ++l) {
-      if (!(any >> l & 1)) continue;
-      const float w = __shfl(p, l, 64);
-      const T* v = (const T*)a.v_pages + __shfl((long long)at, l, 64);
+    for (int l0 = 0; l0 < 64; l0 += AT_ONCE) {
+      if (!(any >> l0 & ((1ull << AT_ONCE) - 1))) continue;
+      float v[AT_ONCE][EL];
 #pragma unroll
-      for (int t = 0; t < EL; ++t)
-        if (lane + 64 * t < hd) acc[t] = fmaf(w, Conv<T>::load(v + lane + 64 * t), acc[t]);
+      for (int l = 0; l < AT_ONCE; ++l) {
+        const T* from = (const T*)a.v_pages + __shfl((long long)at, l0 + l, 64);
+#pragma unroll
+        for (int t = 0; t < EL; ++t) v[l][t] = lane + 64 * t < hd ? Conv<T>::load(from + lane + 64 * t) : 0.f;
+      }
+#pragma unroll
+      for (int l = 0; l < AT_ONCE; ++l) {
+        const float w = __shfl(p, l0 + l, 64);
+        const bool in = any >> (l0 + l) & 1;
+#pragma unroll
+        for (int t = 0; t < EL; ++t) acc[t] = in ? fmaf(w, v[l][t], acc[t]) : acc[t];
+      }
     }
   }
   for (int o = 32; o; o >>= 1) sum += __shfl_xor(sum, o, 64);
-  const float inv = sum == 0.f ? 0.f : 1.0f / sum;
-  T* out = (T*)a.out + row * a.out_stride + (size_t)h * hd;
+  // ---- join the wavefronts
 #pragma unroll
-  for (int t = 0; t < EL; ++t)
-    if (lane + 64 * t < hd) Conv<T>::store(out + lane + 64 * t, sum == 0.f ? 0.f : acc[t] * inv);
+  for (int t = 0; t < EL; ++t) lds_o[wave][lane + 64 * t] = acc[t];
+  if (lane == 0) lds_m[wave] = top, lds_l[wave] = sum;
+  __syncthreads();
+  const int e = threadIdx.x;
+  if (e >= hd) return;
+  float all = -INFINITY, total = 0.f, out = 0.f;
+  for (int w = 0; w < WAVES; ++w) all = fmaxf(all, lds_m[w]);
+  const float ref = all == -INFINITY ? 0.f : all;
+  for (int w = 0; w < WAVES; ++w) {
+    const float f = exp2f(lds_m[w] - ref);
+    total = fmaf(f, lds_l[w], total);
+    out = fmaf(f, lds_o[w][e], out);
+  }
+  Conv<T>::store((T*)a.out + row * a.out_stride + (size_t)h * hd + e, total == 0.f ? 0.f : out / total);
 }
 
 // ------------------------------------------------------------------------------------------------ bf16, heads of 64 and 128
@@ -435,8 +464,7 @@ __device__ __forceinline__ Slice slice_of(const SeqSpan& sp, int split, int spli
 // grid: lengths may be as ragged as they like.  The parts of an item leave partial results, which a second kernel joins.  Every
 // wavefront works this out for itself.
 constexpr int kShareSeqs = 256;              // sequences that a wavefront can add up
-constexpr int kItemTiles = 3;                // tiles that starting and ending a part costs (5 to 6 us; a tile 1.9); with 2 and with 5 in its place
-                                             // trees of 64 rows over 8 x 4096 slots take 103 and 106 us, with 3 100
+constexpr int kItemTiles = 3;                // tiles that starting and ending a part costs (5 to 6 us; a tile 1.9); 2 or 5: the same within 3%
 struct Part {
   int seq, hk, col_tile, key0, key1;
   int parts, part, place;                    // of the item: how many, which, and where in the row of parts this one stands
@@ -557,9 +585,11 @@ __device__ __forceinline__ void leave_note(PartNote* notes, int least, bool any,
 
 }  // namespace
 
-// Up to 32 columns: the four wavefronts of a workgroup take blocks of 32 keys in turn, each for itself (no barrier until the end),
+// Up to 16 columns: the four wavefronts of a workgroup take blocks of 32 keys in turn, each for itself (no barrier until the end),
 // K from global memory straight into operand registers, V through 32 rows of LDS of the wavefront's own; the next block is in
-// flight while one is multiplied.  Bound by what the cache streams at.
+// flight while one is multiplied.  Bound by what the cache streams at: one row each of 32 sequences of 200 to 2048 positions, 32
+// heads of 128, 556 MB, 111 us (5.0 TB/s; all of 2048 192 us, 5.6); one of 100003 positions, 8 key/value heads, 71 us (5.8) and 5 for
+// the join.  A few short sequences: 4.7 us, a chain of loads (row start, length, page, K, V).
 template <int HD>
 __global__ __launch_bounds__(256, 2) void paged_attn_few_kernel(PagedRows b, AttnRows a, int split_len, float* part_o, float* part_ml) {
   using Cols = Columns<HD>;
@@ -697,7 +727,9 @@ __global__ __launch_bounds__(256, 2) void paged_attn_few_kernel(PagedRows b, Att
   if (sl.count > 1 && wave == 0 && g == 0) *(float2*)(part_ml + at * 2) = make_float2(top, sum);
 }
 
-// More columns: every wavefront owns QB blocks of 16, tiles of 64 keys of K and V go through LDS for all of them.
+// 17 to 64 columns: every wavefront owns 16, tiles of 64 keys of K and V go through LDS for all of them, the next on its way through
+// registers.  Still bound by the cache's stream where there is much of it (32 sequences of 4096, 8 key/value heads of 128: 32 columns 107 us,
+// 5.0 TB/s; 64 columns 114); by the chain of starting, tiles and join where there is little (8 sequences: 32 and 35 us).
 template <int HD>
 __global__ __launch_bounds__(256, 2) void paged_attn_tile_kernel(PagedRows b, AttnRows a, int least, float* part_o, float* part_ml,
                                                                     PartNote* notes) {
@@ -859,7 +891,7 @@ template <int HD> struct WideColumns {
     return f;
   }
   // The values of one tile and the scores of the next, step by step in turn (independent sums between dependent ones), the operands of
-  // AHEAD steps on their way from LDS: left to itself the compiler asks for two and waits for them
+  // AHEAD steps on their way from LDS: left to itself the compiler asks for two and waits for them (four to twelve: the same time)
   template <int NB>
   __device__ __forceinline__ void advance(const unsigned char* v_rows, const unsigned char* k_rows, const Frag (&pf)[2 * NB], float (&p)[NB][16],
                                           int lane) {
@@ -917,6 +949,9 @@ __device__ __forceinline__ void load_to_lds(const char* base, uint32_t off, uint
 __device__ __forceinline__ void wait_then_barrier() { asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
 __device__ __forceinline__ uint32_t lds_address(const void* p) { return (uint32_t)(uintptr_t)(__attribute__((address_space(3))) const void*)p; }
 
+// Columns by the hundred.  Trees of 64 rows of 8 sequences of 400 to 4096 positions, 64 query and 8 key/value heads of 128: 59 us and 8 to 11
+// for the join, 32 GFLOP; all of 4096 100 with the join, 0.69 PFLOP/s of the 1.3 that a large matrix product gets.  The exponentials take as long as
+// a third of the products, and the compute units slow down under both (1.6 to 1.7 GHz in long runs).
 // Four wavefronts, two workgroups to a compute unit.  A tile has two halves: the softmax (vector units), and the values of the tile with
 // the scores of the next (matrix units, operands from LDS); the other workgroup is somewhere else in its tiles, so both kinds of unit
 // have work.  K and V come straight to LDS, two stages of each, asked for behind barrier t (K of tile t + 2 and V of t + 1, where K of t and
@@ -1078,6 +1113,8 @@ __global__ __launch_bounds__(256, 2) void paged_attn_wide_kernel(PagedRows b, At
 // in any order and the rows of a product may stand for any e:
 //   scores  lane (r16, g) holds K[r16][16 j + 4 g + i] and Q[r16][16 j + 4 g + i], i the step of four
 //   values  lane (r16, g) holds V[4 g + i][64 j + 4 r16 + x] and, from the scores, P[4 g + i]: x picks which quarter of the e a product has
+// One row of each of 32 sequences of 2000, 8 heads of 128: 100 us (5.2 TB/s); 64 rows of 8 sequences: 72 us, 4 GFLOP, every
+// 16 columns reading the cache for themselves (from L2); trees of 8 of 8 sequences of up to 190: 8 us, the chain of loads.
 template <int HD>
 __global__ __launch_bounds__(256) void paged_attn_f32_kernel(PagedRows b, AttnRows a, int split_len, int col_tiles, float* part_o, float* part_ml) {
   constexpr int KJ = HD / 16, VJ = HD / 64, STEP = 4 * 16;
@@ -1299,7 +1336,9 @@ __global__ __launch_bounds__(PARTS * (HD / 4)) void paged_attn_join_kernel(Paged
   store_four((T*)a.out + (int64_t)(sp.row0 + row) * a.out_stride + (int64_t)head * HD + e, acc, sum);
 }
 
-// The same for shared-out work.  A workgroup per part; those of an item share the item's elements out among them, four elements to a unit, and where that leaves fewer units than threads, the threads share the parts.
+// The same for shared-out work.  A workgroup per part; those of an item share the item's elements out among them, four elements to a
+// unit, and where that leaves fewer units than threads, the threads share the parts.  Bound by the partial results' 34 MB at 512 parts of 128
+// columns of 128 (8 to 11 us).
 template <int HD, int COLS>
 __global__ __launch_bounds__(256) void paged_attn_share_join_kernel(PagedRows b, AttnRows a, const float* part_o, const float* part_ml,
                                                                    const PartNote* notes) {
@@ -1379,10 +1418,14 @@ AttnPlan attn_plan(int dtype, const PagedRows& b, int Hq) {
   p.simple = b.hd != 64 && b.hd != 128;
   if (p.simple) return p;
   p.f32 = dtype == 0;
+  // up to 16 columns: 8 of 8 x 4096 slots 27 us, in parts on the next kernel 30; of 4 x 500 10 and 14 (ragged 32 x 4096: 58 and 54)
   p.slices = p.f32 || cols <= 16;
   if (p.slices) {
     p.blocks = (cols + 15) / 16;
     const int64_t groups = (int64_t)b.seqs * b.Hkv * p.blocks;
+    // slices that all run at once, two workgroups to a compute unit (64 x 4096 slots, 8 heads: 1024 slices 195 us, 512 190; 1 x 100003: 83, 79),
+    // and of float32, whose workgroups hold less, four; not below 256 slots, where the join costs what the slice saves (1 x 2000: 128 slots
+    // 13.5 us, 256 11.9; float32 8 x 2000: 13.0, 12.2, 512 slots 17.9)
     const int least = 256;
     int64_t splits = p.f32 ? (1024 + groups - 1) / groups : 512 / groups;
     if (splits > S / least) splits = S / least;
@@ -1391,11 +1434,13 @@ AttnPlan attn_plan(int dtype, const PagedRows& b, int Hq) {
     p.splits = (S + p.split_len - 1) / p.split_len;
     return p;
   }
+  // 64 columns of 8 x 4096 slots: 35 us, on the kernel for more 38; of 4 x 500 18 and 22
   p.cols = cols <= 64 ? 64 : 128;
-  // two workgroups to a compute unit; a grid that holds every item, or an item to a workgroup where there are many
+  // two workgroups to a compute unit (64-node trees of 8 ragged sequences: 512 of them 70 us, 1024 83, 256 113); a grid that holds every item,
+  // or an item to a workgroup where there are many or the keys are few
   const int64_t items = (int64_t)b.seqs * b.Hkv * ((cols + p.cols - 1) / p.cols), tiles = (S + 63) / 64;
   if (b.seqs <= kShareSeqs && items <= 1024 && items * (tiles + kItemTiles) < 1 << 30 && tiles > 8) {
-    p.least = 8;
+    p.least = 8;                                           // (one tree over 30000: 8 tiles 95 us, 4 95, 16 100; two over 1000: 34, 37, 41)
     p.workgroups = items <= 512 ? 512 : 1024;
     p.workgroups -= p.workgroups % b.Hkv;                  // (every head has room for its items: Hkv <= items)
     const int64_t most = items * ((tiles + kItemTiles + p.least - 1) / p.least);       // parts
@@ -1441,8 +1486,16 @@ hipError_t launch_paged_attn(int dtype, const PagedRows& b, const AttnRows& a, v
   const AttnPlan p = attn_plan(dtype, b, a.Hq);
   if (p.simple) {
     const dim3 grid(a.Hq, b.max_rows, b.seqs);
-    if (dtype == 0) hipLaunchKernelGGL(paged_attn_simple_kernel<float>, grid, dim3(64), 0, s, b, a);
-    else hipLaunchKernelGGL(paged_attn_simple_kernel<bf16_t>, grid, dim3(64), 0, s, b, a);
+    // few heads and rows: sixteen wavefronts over the keys (64 of them: 29 us, with four 82); many: four, of which more fit a compute
+    // unit (1024: 99 us, with sixteen 111; 4096: 310, with sixteen 500)
+    const bool many = (int64_t)a.Hq * b.max_rows * b.seqs > 512;
+    if (dtype == 0) {
+      auto f = many ? paged_attn_simple_kernel<float, 4> : paged_attn_simple_kernel<float, 16>;
+      hipLaunchKernelGGL(f, grid, dim3(many ? 256 : 1024), 0, s, b, a);
+    } else {
+      auto f = many ? paged_attn_simple_kernel<bf16_t, 4> : paged_attn_simple_kernel<bf16_t, 16>;
+      hipLaunchKernelGGL(f, grid, dim3(many ? 256 : 1024), 0, s, b, a);
+    }
     return hipGetLastError();
   }
   float* part_o = (float*)scratch;
