@@ -68,6 +68,29 @@ __device__ inline double exp_series(double y) {
   return e;
 }
 
+// The value of lane ^ STRIDE by moves that need no LDS
+template <int CTRL> __device__ inline uint32_t dpp(uint32_t v) { return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, CTRL, 0xf, 0xf, false); }
+template <int STRIDE> __device__ inline uint32_t of_partner(uint32_t v) {
+  if constexpr (STRIDE == 1) return dpp<0xb1>(v);          // quads 1 0 3 2
+  if constexpr (STRIDE == 2) return dpp<0x4e>(v);          // quads 2 3 0 1
+  if constexpr (STRIDE == 4) return dpp<0x1b>(dpp<0x141>(v));          // mirrored halves of a row (^ 7), then mirrored quads (^ 3)
+  if constexpr (STRIDE == 8) return dpp<0x128>(v);         // rows turned by 8
+  if constexpr (STRIDE == 16) {
+    const auto r = __builtin_amdgcn_permlane16_swap(v, v, false, false);         // (rows 0 0 2 2, rows 1 1 3 3)
+    return threadIdx.x & 16 ? r[0] : r[1];
+  }
+  if constexpr (STRIDE == 32) {
+    const auto r = __builtin_amdgcn_permlane32_swap(v, v, false, false);
+    return threadIdx.x & 32 ? r[0] : r[1];
+  }
+}
+// A step of a bitonic sort between lanes STRIDE apart
+template <int STRIDE> __device__ inline void sort_step(unsigned long long& key, bool up) {
+  const unsigned long long other = (unsigned long long)of_partner<STRIDE>((uint32_t)(key >> 32)) << 32 | of_partner<STRIDE>((uint32_t)key);
+  const bool first = (threadIdx.x & STRIDE) == 0;
+  key = (other < key) == (up == first) ? other : key;
+}
+
 // Sums and extremes over a wavefront by DPP moves: lane 63 ends with all (a lane that has no partner takes `none`)
 template <int CTRL, int ROWS, typename V> __device__ inline V moved(V v, V none) {
   if constexpr (sizeof(V) == 4) {
@@ -298,21 +321,24 @@ __global__ __launch_bounds__(kThreads) void sample_rows_kernel(SampleRows a) {
       int size = 512;
       while (size < n) size *= 2;
       unsigned long long key = tid < n ? loose[tid] : ~0ull;
-      for (int half = 2; half <= size; half *= 2)
-        for (int stride = half / 2; stride; stride /= 2) {
-          unsigned long long other;
-          if (stride >= 64) {
-            __syncthreads();
-            if (tid < size) keys[tid] = key;
-            __syncthreads();
-            other = tid < size ? keys[tid ^ stride] : 0;
-          } else {
-            if (wave * 64 >= size) continue;
-            other = __shfl_xor(key, stride, 64);
-          }
-          const bool up = (tid & half) == 0, first = (tid & stride) == 0;
+      for (int half = 2; half <= size; half *= 2) {
+        const bool up = (tid & half) == 0;
+        for (int stride = half / 2; stride >= 64; stride /= 2) {
+          __syncthreads();
+          if (tid < size) keys[tid] = key;
+          __syncthreads();
+          const unsigned long long other = tid < size ? keys[tid ^ stride] : 0;
+          const bool first = (tid & stride) == 0;
           key = (other < key) == (up == first) ? other : key;
         }
+        if (wave * 64 >= size) continue;
+        if (half > 32) sort_step<32>(key, up);
+        if (half > 16) sort_step<16>(key, up);
+        if (half > 8) sort_step<8>(key, up);
+        if (half > 4) sort_step<4>(key, up);
+        if (half > 2) sort_step<2>(key, up);
+        sort_step<1>(key, up);
+      }
       __syncthreads();
       if (tid < size) keys[tid] = key;
     }
