@@ -274,12 +274,13 @@ def _current_device() -> int:
         return torch.cuda.current_device()
 
 
-def _empty(shape, dtype, device, stream):
-    """Memory for a call on `stream`: the allocator's, for that stream (what another stream has freed may still be in use there)."""
+def _empty(like, shape, dtype, stream):
+    """Memory on the device of `like` for a call on `stream`: the allocator's, for that stream (what another stream has freed may still
+    be in use there).  (torch.empty with a device takes twice as long.)"""
     if stream is None:
-        return torch.empty(shape, dtype=dtype, device=device)
+        return like.new_empty(shape, dtype=dtype)
     with torch.cuda.stream(stream):
-        return torch.empty(shape, dtype=dtype, device=device)
+        return like.new_empty(shape, dtype=dtype)
 
 
 _DTYPES = {torch.float32: HT_F32, torch.bfloat16: HT_BF16}
@@ -308,7 +309,7 @@ class PagedBatch:
         c.len = _need(length, "length", torch.int32, (self.seqs,), self.device)
         c.page_table = _need(page_table, "page_table", torch.int32, page_table.shape, self.device)
         self.ref = C.byref(c)
-        self.tensors = (row_start, length, page_table)          # kept alive
+        self.like, self.tensors = row_start, (row_start, length, page_table)          # kept alive
 
     def pages(self, t, name):
         return _need(t, name, self.dtype, self.pool, self.device)
@@ -333,8 +334,8 @@ def ht_tree_tables(batch: PagedBatch, parent, stream=None):
     """(depth [rows] int32, anc [rows, HT_MAX_ROWS // 64] int64) of parent [rows] int32."""
     if parent is None:
         raise _bad("parent is None")
-    depth = _empty((batch.rows,), torch.int32, batch.device, stream)
-    anc = _empty((batch.rows, HT_MAX_ROWS // 64), torch.int64, batch.device, stream)
+    depth = _empty(batch.like, (batch.rows,), torch.int32, stream)
+    anc = _empty(batch.like, (batch.rows, HT_MAX_ROWS // 64), torch.int64, stream)
     _run(batch.device, stream, lib.ht_tree_tables, batch.ref, batch.ints(parent, "parent"), depth.data_ptr(), anc.data_ptr())
     return depth, anc
 
@@ -346,7 +347,7 @@ def ht_paged_append(batch: PagedBatch, q, k, v, k_pages, v_pages, depth=None, q_
     hd = batch.pool[3]
     rot = hd if rot is None else rot
     if q is not None and q_out is None:
-        q_out = _empty(q.shape, q.dtype, q.device, stream)
+        q_out = _empty(q, q.shape, q.dtype, stream)
     (qp, qs), (kp, ks), (vp, vs), (op, os_) = (batch.heads(t, n) for t, n in ((q, "q"), (k, "k"), (v, "v"), (q_out, "q_out")))
     if q is not None and q.shape != q_out.shape:
         raise _bad("q_out has another shape than q")
@@ -367,7 +368,7 @@ def ht_paged_attention_scratch_bytes(batch: PagedBatch, Hq: int) -> int:
 
 def ht_paged_attention_scratch(batch: PagedBatch, Hq: int, stream=None):
     """Scratch of a size for `ht_paged_attention` (one for every call that may run at the same time)."""
-    return _empty((max(256, ht_paged_attention_scratch_bytes(batch, Hq)),), torch.uint8, batch.device, stream)
+    return _empty(batch.like, (max(256, ht_paged_attention_scratch_bytes(batch, Hq)),), torch.uint8, stream)
 
 
 def ht_paged_attention(batch: PagedBatch, q, k_pages, v_pages, anc=None, scale=None, out=None, scratch=None, stream=None):
@@ -376,7 +377,7 @@ def ht_paged_attention(batch: PagedBatch, q, k_pages, v_pages, anc=None, scale=N
     if q is None:
         raise _bad("q is None")
     if out is None:
-        out = _empty(q.shape, q.dtype, q.device, stream)
+        out = _empty(q, q.shape, q.dtype, stream)
     (qp, qs), (op, os_) = batch.heads(q, "q"), batch.heads(out, "out")
     if q.shape != out.shape:
         raise _bad("out has another shape than q")
@@ -403,9 +404,9 @@ def ht_sample_rows(logits, u, temperature=None, top_k=None, top_p=None, min_p=No
         raise _bad("u is None")
     f, i = torch.float32, torch.int32
     if tokens is None:
-        tokens = _empty((rows,), i, dev, stream)
+        tokens = _empty(logits, (rows,), i, stream)
     if logprob is None:
-        logprob = _empty((rows,), f, dev, stream)
+        logprob = _empty(logits, (rows,), f, stream)
     _run(dev, stream, lib.ht_sample_rows, logits.data_ptr(), logits.stride(0) if rows > 1 else V, _DTYPES[logits.dtype], rows, V,
          _need(u, "u", f, (rows,), dev), _need(temperature, "temperature", f, (rows,), dev), _need(top_k, "top_k", i, (rows,), dev),
          _need(top_p, "top_p", f, (rows,), dev), _need(min_p, "min_p", f, (rows,), dev), _need(tokens, "tokens", i, (rows,), dev),
@@ -426,12 +427,12 @@ def ht_paged_accept(batch: PagedBatch, k_pages, v_pages, parent, tokens, answers
     if P < 1 or P > HT_MAX_ROWS:
         raise _bad(f"max_path {P} outside 1..{HT_MAX_ROWS}")
     if out is None:
-        out = _empty((3 * B + 2 * B * P,), torch.int32, batch.device, stream)
+        out = _empty(batch.like, (3 * B + 2 * B * P,), torch.int32, stream)
     at = _need(out, "out", torch.int32, (3 * B + 2 * B * P,), batch.device)
     _run(batch.device, stream, lib.ht_paged_accept, batch.ref, layers, k_pages.stride(0) if layers > 1 else 0, kp, vp,
          batch.ints(parent, "parent"), batch.ints(tokens, "tokens"), batch.ints(answers, "answers"), P, at, at + 12 * B,
          at + 12 * B + 4 * B * P, at + 4 * B, at + 8 * B)
-    n, root, length, path, emitted = out.split([B, B, B, B * P, B * P])
+    n, root, length, path, emitted = torch.split_with_sizes(out, [B, B, B, B * P, B * P])
     return n, path.view(B, P), emitted.view(B, P), root, length
 
 
