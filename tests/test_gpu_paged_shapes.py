@@ -254,3 +254,52 @@ def test_the_largest_vocabulary_and_many_rows():
     z = torch.randn(rows, 5, generator=g)
     tokens, lp = B.ht_sample_rows(z.to(DEV), torch.rand(rows, generator=g).to(DEV), top_k=torch.ones(rows, dtype=torch.int32, device=DEV))
     assert torch.equal(tokens.cpu().long(), z.argmax(1)) and (lp == 0).all()
+
+
+@pytest.mark.parametrize("Hkv,seqs,rows", [(300, 1, 40), (700, 1, 20), (5, 3, 100), (48, 2, 70)])
+def test_heads_that_do_not_divide_the_grid(Hkv, seqs, rows):
+    attend(Case([1500, 600, 40][:seqs], [rows, 3, rows][:seqs], Hkv, 64, 64, BF16, 50), Hkv, f"{Hkv} heads, {rows} rows")
+
+
+@pytest.mark.parametrize("dtype,rows,hd", [(F32, 20, 64), (BF16, 2, 128), (BF16, 12, 128), (BF16, 100, 64), (BF16, 5, 80)])
+def test_a_batch_that_has_nothing_to_do(dtype, rows, hd):
+    """No sequence has rows: nothing is written, by any of the calls but the lengths."""
+    B = _B()
+    case = Case([3000, 0], [rows, rows], 2, hd, 16, dtype, 51)
+    pools = [p.to(DEV) for p in case.new_pools()]
+    case.starts = [0, 0, 0]
+    batch = case.batch(B, pools)
+    q, k = (torch.ones(case.rows, h, hd, dtype=dtype, device=DEV) for h in (8, 2))
+    before = [p.cpu().clone() for p in pools]
+    out = torch.full_like(q, 77.0)
+    B.ht_paged_attention(batch, q, *pools, case.anc().to(DEV), out=out)
+    B.ht_paged_append(batch, q, k, k, *pools, q_out=out)
+    ints = torch.zeros(case.rows, dtype=torch.int32, device=DEV)
+    n, path, emitted, root, length = B.ht_paged_accept(batch, *pools, ints, ints, ints, 4)
+    assert (out == 77.0).all() and n.tolist() == [0, 0] and root.tolist() == [-1, -1] and length.tolist() == [3000, 0]
+    assert (path == -1).all() and (emitted == -1).all()
+    as_int = torch.int16 if dtype == BF16 else torch.int32
+    for p, x in zip(pools, before):
+        assert torch.equal(p.cpu().view(as_int), x.view(as_int))
+
+
+@pytest.mark.parametrize("dtype,rows", [(F32, 20), (BF16, 4), (BF16, 12), (BF16, 100)])
+def test_two_calls_at_once(dtype, rows):
+    """On two streams, each with scratch of its own: the bits of calls by themselves."""
+    B = _B()
+    cases = [Case([2500, 700], [rows, rows], 2, 128, 32, dtype, 52 + i) for i in range(2)]
+    work = []
+    for case in cases:
+        pools = [p.to(DEV) for p in case.new_pools()]
+        q = case.normal(case.rows, 8, 128).to(DEV)
+        batch, anc = case.batch(B, pools), case.anc().to(DEV)
+        work.append((batch, q, pools, anc, B.ht_paged_attention(batch, q, *pools, anc), B.ht_paged_attention_scratch(batch, 8), torch.cuda.Stream()))
+        check(case, work[-1][4], q, pools, "alone")
+    outs = [torch.empty_like(w[1]) for w in work]
+    torch.cuda.synchronize()
+    for _ in range(10):
+        for o, (batch, q, pools, anc, _want, scratch, stream) in zip(outs, work):
+            B.ht_paged_attention(batch, q, *pools, anc, out=o, scratch=scratch, stream=stream)
+    torch.cuda.synchronize()
+    for o, w in zip(outs, work):
+        assert torch.equal(o, w[4])
